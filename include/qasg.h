@@ -20,6 +20,10 @@
  *   - One context must not be used from two streams at the same time: its workspace
  *     (per-worker statistics, partial sums, code scratch) is shared by all calls.
  *   - Step index t is 1-based.  1 <= M <= 64.  1 <= d <= 2^34.
+ *   - The language-model operators (qasg_act_*, qasg_rmsnorm_*, qasg_token_logprob*) take the element
+ *     type of their tensors as a qasg_dtype; pointers to such tensors need that type's alignment only,
+ *     and 16-byte alignment of rows is faster.  They use the context for its device, its status word
+ *     and its launch count: their sizes are not bound by d_max and M_max.
  *   - There is no CPU implementation behind this interface.
  */
 #ifndef QASG_H_
@@ -354,6 +358,118 @@ qasg_status qasg_quantize_pack_optimal(qasg_ctx* ctx, const float* g, uint64_t d
                                        float* thresholds, uint64_t* counts, void* scratch,
                                        uint64_t scratch_bytes, void* stream);
 
+/* ---------------------------------------------------------------- language-model operators
+ * What the last block and the head of a language model need to produce the workers' gradient rows g
+ * that the steps above consume: the norm in front of a linear layer with its output kept in 8 bits, the
+ * layer's weight gradient taken from those 8 bits, and the log probabilities that the loss is made of.
+ * (The paper trains its models elsewhere; these entry points stand beside the logistic-regression
+ * gradients, for models whose rows of g are weight matrices.) */
+typedef enum { QASG_F32 = 0, QASG_BF16 = 1, QASG_F16 = 2 } qasg_dtype;
+
+/* A matrix of activations kept in 8 bits (device memory owned by the caller).  Blocks of QASG_ACT_BLOCK
+ * values along a row share one exponent E = max(floor(log2 max|a|), -120), stored as the byte E + 127; a
+ * value's code is a * 2^(6-E) rounded to the nearest integer, ties to even, within [-127, 127], and stands
+ * for code * 2^(E-6), which is exact in bf16 and fp32.  (The integer element and the power-of-two scale of
+ * the OCP Microscaling formats, MXINT8.)  The last block of a row may be short; its unused codes are 0.
+ * A block that holds an infinity or a NaN gets the byte 255, codes 0, and stands for NaNs. */
+#define QASG_ACT_BLOCK 32u
+typedef struct {
+  uint32_t struct_size; /* sizeof(qasg_act), checked                                            */
+  uint32_t cols;        /* values of a row, 1 .. 2^20                                           */
+  uint64_t rows;        /* 0 .. 2^31 - 1                                                        */
+  int8_t* codes;        /* [rows][ld_codes], 16-byte aligned                                    */
+  uint8_t* exps;        /* [rows][ld_exps], 16-byte aligned                                     */
+  uint64_t ld_codes;    /* a multiple of 32, >= cols                                            */
+  uint64_t ld_exps;     /* a multiple of 16, >= ceil(cols / 32)                                 */
+} qasg_act;
+
+/* Fills the checkpoint act with x (dtype, [rows][ld_x], ld_x >= cols).  A non-finite value is reported as
+ * QASG_ERR_NONFINITE by qasg_last_async_status. */
+qasg_status qasg_act_pack(qasg_ctx* ctx, qasg_dtype dtype, const void* x, uint64_t ld_x, const qasg_act* act,
+                          void* stream);
+/* Writes the values that act stands for to x (dtype, [rows][ld_x]); f32 and bf16 hold them exactly, f16
+ * rounds (to an infinity above 65504). */
+qasg_status qasg_act_unpack(qasg_ctx* ctx, const qasg_act* act, qasg_dtype dtype, void* x, uint64_t ld_x,
+                            void* stream);
+
+/* Weight gradient of a linear layer whose input was kept in act, for M workers at once: the rows of dy and
+ * act from shard_row0[m] to shard_row0[m+1] - 1 belong to worker m, and
+ *   g[m*ld_g + n*ld_w + k] (+)= weight_k * sum over those rows r of dy[r][n] * a^[r][k],
+ * a^ being the values that act stands for.  The products are exact and the sums are taken in fp32 in an
+ * order that depends on the sizes alone.  A worker without rows gets zeros.
+ *   dy         device, dtype [rows][ld_dy], ld_dy >= out_cols: the gradient of the layer's output.
+ *   weight     device, fp32 [cols] or NULL: one factor per column (the norm's weight, when act holds the
+ *              normalised values without it).
+ *   shard_row0 host, uint64 [M+1], from 0 to act->rows, not decreasing; 1 <= M <= 64.
+ *   g          device, fp32; ld_w >= cols, ld_g >= (out_cols-1)*ld_w + cols: row m of a gradient array
+ *              [M][ld_g] at the layer's place in it.
+ *   accumulate 0: overwrite; else add to what g holds.
+ *   scratch    device, 16-byte aligned, qasg_act_wgrad_scratch_bytes(out_cols, cols, M) bytes, which does
+ *              not depend on the rows; contents undefined afterwards. */
+uint64_t qasg_act_wgrad_scratch_bytes(uint64_t out_cols, uint64_t cols, uint32_t M);
+qasg_status qasg_act_wgrad(qasg_ctx* ctx, qasg_dtype dtype, const void* dy, uint64_t ld_dy, uint64_t out_cols,
+                           const qasg_act* act, const float* weight, uint32_t M, const uint64_t* shard_row0,
+                           float* g, uint64_t ld_g, uint64_t ld_w, int accumulate, void* scratch,
+                           uint64_t scratch_bytes, void* stream);
+
+/* Root-mean-square norm with the residual's addition and its output in 8 bits:
+ *   h = x + residual;  rstd = 1 / sqrt(mean of h^2 over the row + eps);  act = 8-bit form of n = h * rstd;
+ *   y = weight * n^, with n^ the values that act stands for
+ * (so what the next layer reads is what the checkpoint holds).  Arithmetic in fp32 from the unrounded h.
+ * act and rstd are all the gradient needs.  rows = act->rows, cols = act->cols <= 16384.
+ *   x, residual  device, dtype [rows][ld]; residual may be NULL (h = x).
+ *   weight       device, fp32 [cols] or NULL (ones).      eps  >= 0.
+ *   h, y         device, dtype [rows][ld], each may be NULL.  h may be x or residual itself, with the
+ *                same leading dimension.
+ *   rstd         device, fp32 [rows].
+ * A row of zeros with eps = 0, or a non-finite value, is reported as QASG_ERR_NONFINITE. */
+qasg_status qasg_rmsnorm_pack(qasg_ctx* ctx, qasg_dtype dtype, const void* x, uint64_t ld_x, const void* residual,
+                              uint64_t ld_r, const float* weight, float eps, void* h, uint64_t ld_h, void* y,
+                              uint64_t ld_y, const qasg_act* act, float* rstd, void* stream);
+
+/* Its gradient, the rounding to 8 bits taken as the identity, for M workers at once (shards as above):
+ *   u = weight * dy;  dx = dres + rstd * (u - n^ * mean of u * n^ over the row)
+ *   gw[m*ld_g + k] (+)= sum over the rows r of worker m of dy[r][k] * n^[r][k]
+ * dx is the gradient of x and of residual alike.
+ *   dy, dres  device, dtype [rows][ld]; dres, the gradient that reaches h by the residual path, may be NULL.
+ *   dx        device, dtype [rows][ld_dx]; may be dy or dres itself, with the same leading dimension.
+ *   gw        device, fp32, ld_g >= cols when M > 1; NULL: not wanted.
+ *   scratch   device, 16-byte aligned, qasg_rmsnorm_grad_scratch_bytes(cols, M) bytes; may be NULL when gw is. */
+uint64_t qasg_rmsnorm_grad_scratch_bytes(uint64_t cols, uint32_t M);
+qasg_status qasg_rmsnorm_grad(qasg_ctx* ctx, qasg_dtype dtype, const void* dy, uint64_t ld_dy, const void* dres,
+                              uint64_t ld_dres, const qasg_act* act, const float* rstd, const float* weight,
+                              uint32_t M, const uint64_t* shard_row0, void* dx, uint64_t ld_dx, float* gw,
+                              uint64_t ld_g, int accumulate, void* scratch, uint64_t scratch_bytes, void* stream);
+
+/* Per row of logits x (dtype, [rows][ld], ld >= vocab, 1 <= vocab < 2^31, 1 <= rows < 2^31):
+ *   lse = log sum_v exp(x_v);  logprob = x_token - lse;  entropy = -sum_v p_v log p_v, p = exp(x - lse);
+ *   top_ids, top_logprob: the k columns of the largest logits, largest first, of equal ones the lowest
+ *   column first, and x - lse there.
+ * Logits of -inf are tokens that are masked out.  A row of nothing else has lse, logprob and top_logprob
+ * -inf and entropy 0.  A row with a NaN or +inf gets NaNs (top_ids: NaN counts as the largest value) and is
+ * reported as QASG_ERR_NONFINITE.
+ *   tokens       device, int64 [rows] or NULL.  A row whose token is negative is padding: it is not read, its
+ *                outputs are 0, its top_ids -1; a token >= vocab is treated the same way and reported as
+ *                QASG_ERR_BAD_INDEX.
+ *   logprob, entropy, lse   device, fp32 [rows], each may be NULL; logprob needs tokens.
+ *   k            0 .. min(vocab, QASG_TOP_MAX).
+ *   top_ids, top_logprob    device, int64 and fp32 [rows][k], each may be NULL. */
+#define QASG_TOP_MAX 32u
+qasg_status qasg_token_logprob(qasg_ctx* ctx, qasg_dtype dtype, const void* logits, uint64_t ld, uint64_t rows,
+                               uint64_t vocab, const int64_t* tokens, float* logprob, float* entropy, float* lse,
+                               uint32_t k, int64_t* top_ids, float* top_logprob, void* stream);
+
+/* The gradient of the logits, from lse and entropy as written by qasg_token_logprob and the gradients of
+ * the three per-row outputs (device, fp32 [rows], each may be NULL for zeros; entropy may be NULL when
+ * g_entropy is):
+ *   dlogits_v = p_v * (g_lse - g_logprob - g_entropy * (log p_v + entropy)) + [v = token] * g_logprob.
+ * Padding rows and rows of nothing but -inf get zeros.  tokens NULL: no token is given, g_logprob is not used.
+ *   dlogits  device, dtype [rows][ld_d]; may be logits itself, with the same leading dimension. */
+qasg_status qasg_token_logprob_grad(qasg_ctx* ctx, qasg_dtype dtype, const void* logits, uint64_t ld, uint64_t rows,
+                                    uint64_t vocab, const int64_t* tokens, const float* lse, const float* entropy,
+                                    const float* g_logprob, const float* g_entropy, const float* g_lse,
+                                    void* dlogits, uint64_t ld_d, void* stream);
+
 /* The threshold quantizer of qasg_quantize_pack for callers that cannot allocate device
  * memory.  (The paper has no counterpart: this entry point exists for the sake of its
  * callers, not of the method.)
@@ -403,7 +519,7 @@ uint64_t qasg_launch_count(const qasg_ctx* ctx);
  * adds up, per kernel id (0 <= id < QASG_KERNEL_COUNT, names from qasg_kernel_name), the
  * elapsed milliseconds into ms[id] and the number of launches into launches[id] (both host
  * arrays of QASG_KERNEL_COUNT entries), then stops recording. */
-#define QASG_KERNEL_COUNT 26
+#define QASG_KERNEL_COUNT 33
 qasg_status qasg_profile_begin(qasg_ctx* ctx);
 qasg_status qasg_profile_end(qasg_ctx* ctx, double* ms, uint64_t* launches);
 const char* qasg_kernel_name(int id);

@@ -8,8 +8,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "lib", "libqasg.so")
 SOURCES = ["qasg_api.cu", "qasg_kernels.cu", "qasg_logreg.cu", "qasg_static.cu", "qasg_optimal.cu", "qasg_touched.cu",
-           "qasg_stream.cu"]
-HEADERS = [os.path.join(CSRC, "qasg_internal.h"), os.path.join(CSRC, "qasg_device.cuh"),
+           "qasg_stream.cu", "qasg_act.cu", "qasg_norm.cu", "qasg_wgrad.cu", "qasg_logprob.cu"]
+HEADERS = [os.path.join(CSRC, "qasg_internal.h"), os.path.join(CSRC, "qasg_device.cuh"), os.path.join(CSRC, "qasg_lm.cuh"),
            os.path.join(os.path.dirname(HERE), "include", "qasg.h")]
 
 
@@ -34,7 +34,7 @@ def build_library(force=False, verbose=False):
         return LIB
     os.makedirs(os.path.dirname(LIB), exist_ok=True)
     cmd = [_nvcc(), "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-           "-shared", "-Xcompiler", "-fPIC", "-o", LIB] + [os.path.join(CSRC, s) for s in SOURCES]
+           "--threads", "0", "-shared", "-Xcompiler", "-fPIC", "-o", LIB] + [os.path.join(CSRC, s) for s in SOURCES]
     if verbose:
         cmd.insert(1, "-Xptxas")
         cmd.insert(2, "-v")

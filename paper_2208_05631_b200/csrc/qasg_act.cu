@@ -1,0 +1,117 @@
+// 8-bit activation checkpoints: packing and restoring.  Both move every value once (elementwise work on blocks
+// of 32), so HBM bounds them: a warp takes 1024 columns of a row, a lane four units of eight values, all its
+// loads in flight together; the four lanes of a block find its largest magnitude with two shuffles.
+#include "qasg_lm.cuh"
+
+namespace qasg {
+
+constexpr int kActItemUnits = 4;                                  // units a lane owns, 32 apart
+constexpr int kActItem = kActItemUnits * 32 * kUnit;              // columns of one warp's item
+constexpr int kActWarps = 8;
+
+struct ActItem {
+  uint64_t row;
+  uint32_t col;  // first column of the item
+};
+__device__ __forceinline__ ActItem act_item(uint64_t item, uint32_t per_row) {
+  ActItem a;
+  if (item >> 32) {
+    a.row = item / per_row;
+    a.col = static_cast<uint32_t>(item - a.row * per_row) * kActItem;
+  } else {
+    const uint32_t r = static_cast<uint32_t>(item) / per_row;
+    a.row = r;
+    a.col = (static_cast<uint32_t>(item) - r * per_row) * kActItem;
+  }
+  return a;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kActWarps * 32)
+act_pack_kernel(const T* __restrict__ x, uint64_t ld_x, ActView act, uint64_t items, uint32_t per_row,
+                unsigned int* __restrict__ status) {
+  const uint64_t item = static_cast<uint64_t>(blockIdx.x) * kActWarps + (threadIdx.x >> 5);
+  const uint32_t lane = threadIdx.x & 31;
+  chain_wait();
+  chain_trigger();
+  if (item >= items) return;
+  const ActItem a = act_item(item, per_row);
+  const T* row = x + a.row * ld_x;
+  const uint32_t padded = (act.cols + kActBlock - 1) & ~static_cast<uint32_t>(kActBlock - 1);
+  float v[kActItemUnits][kUnit];
+#pragma unroll
+  for (int j = 0; j < kActItemUnits; ++j)
+    load_values<T>(row, a.col + (j * 32 + lane) * kUnit, act.cols, 0.f, v[j]);
+  bool bad = false;
+#pragma unroll
+  for (int j = 0; j < kActItemUnits; ++j) {
+    const uint32_t c = a.col + (j * 32 + lane) * kUnit;
+    const uint32_t b = act_exponent(block_largest(v[j]));
+    const uint2 codes = act_codes(v[j], b);
+    if (c < padded) {
+      *reinterpret_cast<uint2*>(act.codes + a.row * act.ld_codes + c) = codes;
+      if ((lane & 3) == 0) act.exps[a.row * act.ld_exps + c / kActBlock] = static_cast<uint8_t>(b);
+      bad |= b == kActNan;
+    }
+  }
+  if (bad) atomicOr(status, kFlagNonFinite);
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kActWarps * 32)
+act_unpack_kernel(ActView act, T* __restrict__ x, uint64_t ld_x, uint64_t items, uint32_t per_row) {
+  const uint64_t item = static_cast<uint64_t>(blockIdx.x) * kActWarps + (threadIdx.x >> 5);
+  const uint32_t lane = threadIdx.x & 31;
+  chain_wait();
+  chain_trigger();
+  if (item >= items) return;
+  const ActItem a = act_item(item, per_row);
+  uint2 codes[kActItemUnits];
+  uint32_t exps[kActItemUnits];
+#pragma unroll
+  for (int j = 0; j < kActItemUnits; ++j) {
+    const uint32_t c = a.col + (j * 32 + lane) * kUnit;
+    if (c >= act.cols) continue;
+    codes[j] = __ldcs(reinterpret_cast<const uint2*>(act.codes + a.row * act.ld_codes + c));
+    exps[j] = act.exps[a.row * act.ld_exps + c / kActBlock];
+  }
+#pragma unroll
+  for (int j = 0; j < kActItemUnits; ++j) {
+    const uint32_t c = a.col + (j * 32 + lane) * kUnit;
+    if (c >= act.cols) continue;
+    float v[kUnit];
+    code_floats(codes[j], v);
+    const float unit = act_unit(exps[j]);
+#pragma unroll
+    for (int k = 0; k < kUnit; ++k) v[k] *= unit;
+    store_values<T>(x + a.row * ld_x, c, act.cols, v);
+  }
+}
+
+int launch_act_pack(int dtype, const void* x, uint64_t ld_x, const ActView& act, unsigned int* status,
+                    const LaunchShape& shape, cudaStream_t stream) {
+  const uint32_t per_row = (act.cols + kActItem - 1) / kActItem;
+  const uint64_t items = act.rows * per_row;
+  const dim3 grid(static_cast<unsigned>((items + kActWarps - 1) / kActWarps));
+  with_dtype(dtype, [&](auto t) {
+    using T = decltype(t);
+    launch_lm(act_pack_kernel<T>, grid, kActWarps * 32, 0, 1, stream, shape.chained, static_cast<const T*>(x), ld_x, act,
+              items, per_row, status);
+  });
+  return 1;
+}
+
+int launch_act_unpack(const ActView& act, int dtype, void* x, uint64_t ld_x, const LaunchShape& shape,
+                      cudaStream_t stream) {
+  const uint32_t per_row = (act.cols + kActItem - 1) / kActItem;
+  const uint64_t items = act.rows * per_row;
+  const dim3 grid(static_cast<unsigned>((items + kActWarps - 1) / kActWarps));
+  with_dtype(dtype, [&](auto t) {
+    using T = decltype(t);
+    launch_lm(act_unpack_kernel<T>, grid, kActWarps * 32, 0, 1, stream, shape.chained, act, static_cast<T*>(x), ld_x, items,
+              per_row);
+  });
+  return 1;
+}
+
+}  // namespace qasg

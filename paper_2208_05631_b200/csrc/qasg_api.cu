@@ -43,7 +43,8 @@ enum KernelId {
   kDecodeAverage, kDenseUpdateCmd, kDenseUpdateRda, kLogregDense, kLogregCsr, kAvgAbsSum, kAvgAbsMax,
   kAvgThresholdCodes, kAvgStochasticCodes, kSelectStats, kIndicatorOr, kTouchedClear, kLogregCsrTouched,
   kOptimalThreshold, kMeanUpdateCmd, kMeanUpdateRda, kStreamThreshold, kStreamStochastic, kFusedStepCmd,
-  kFusedStepRda, kKernelIdCount
+  kFusedStepRda, kActPack, kActUnpack, kActWgrad, kRmsnormPack, kRmsnormGrad, kTokenLogprob, kTokenLogprobGrad,
+  kKernelIdCount
 };
 static_assert(kKernelIdCount <= QASG_KERNEL_COUNT, "kernel id table");
 
@@ -293,6 +294,41 @@ qasg_status check_step(const qasg_ctx* ctx, int rule, const float* g, uint64_t d
   if (!aligned16(x) || !aligned16(h) || (z && !aligned16(z)) || (codes_out && !aligned16(codes_out)))
     return QASG_ERR_ALIGNMENT;
   if (params->quantizer != QASG_Q_NONE && !codes_out && !ctx->code_scratch) return QASG_ERR_WORKSPACE;
+  return QASG_OK;
+}
+
+// ------------------------------------------------------------------ language-model operators
+constexpr uint64_t kMaxRows = (1ull << 31) - 1;
+constexpr uint32_t kActMaxCols = 1u << 20;
+static_assert(QASG_ACT_BLOCK == 32 && QASG_TOP_MAX == kMaxTop, "header");
+
+// A tensor of rows with leading dimension ld; NULL only where there are no rows.
+qasg_status check_rows(int dtype, const void* p, uint64_t ld, uint64_t rows, uint64_t cols) {
+  if (dtype != QASG_F32 && dtype != QASG_BF16 && dtype != QASG_F16) return QASG_ERR_INVALID_ARG;
+  if ((!p && rows) || ld < cols || ld > (1ull << 40)) return QASG_ERR_INVALID_ARG;
+  return reinterpret_cast<uintptr_t>(p) % (dtype == QASG_F32 ? 4 : 2) ? QASG_ERR_ALIGNMENT : QASG_OK;
+}
+
+qasg_status check_floats(const float* p) { return reinterpret_cast<uintptr_t>(p) & 3u ? QASG_ERR_ALIGNMENT : QASG_OK; }
+
+qasg_status check_act(const qasg_act* act, ActView* view) {
+  if (!act || act->struct_size != sizeof(qasg_act)) return QASG_ERR_INVALID_ARG;
+  if (act->cols < 1 || act->cols > kActMaxCols || act->rows > kMaxRows) return QASG_ERR_INVALID_ARG;
+  if ((!act->codes || !act->exps) && act->rows) return QASG_ERR_INVALID_ARG;
+  if (act->ld_codes < act->cols || act->ld_exps < (act->cols + 31u) / 32u) return QASG_ERR_INVALID_ARG;
+  if (act->ld_codes > (1ull << 32) || act->ld_exps > (1ull << 32)) return QASG_ERR_INVALID_ARG;
+  if ((act->ld_codes & 31u) || (act->ld_exps & 15u) || !aligned16(act->codes) || !aligned16(act->exps))
+    return QASG_ERR_ALIGNMENT;
+  *view = {act->codes, act->exps, act->rows, act->ld_codes, act->ld_exps, act->cols};
+  return QASG_OK;
+}
+
+qasg_status check_row_shards(uint32_t M, const uint64_t* shard_row0, uint64_t rows, RowShards* shards) {
+  if (M < 1 || M > static_cast<uint32_t>(kMaxWorkers) || !shard_row0) return QASG_ERR_INVALID_ARG;
+  if (shard_row0[0] != 0 || shard_row0[M] != rows) return QASG_ERR_INVALID_ARG;
+  for (uint32_t m = 0; m < M; ++m)
+    if (shard_row0[m + 1] < shard_row0[m]) return QASG_ERR_INVALID_ARG;
+  for (uint32_t m = 0; m <= static_cast<uint32_t>(kMaxWorkers); ++m) shards->row0[m] = shard_row0[m < M ? m : M];
   return QASG_OK;
 }
 
@@ -812,6 +848,171 @@ qasg_status qasg_logreg_grad_csr_touched(qasg_ctx* ctx, const int64_t* rowptr, c
   return leave(ctx);
 }
 
+qasg_status qasg_act_pack(qasg_ctx* ctx, qasg_dtype dtype, const void* x, uint64_t ld_x, const qasg_act* act,
+                          void* stream) {
+  ActView view;
+  qasg_status st = ctx ? check_act(act, &view) : QASG_ERR_INVALID_ARG;
+  if (st == QASG_OK) st = check_rows(dtype, x, ld_x, view.rows, view.cols);
+  if (st != QASG_OK || !view.rows) return st;
+  if ((st = enter(ctx)) != QASG_OK) return st;
+  {
+    Launch l(ctx, kActPack, static_cast<cudaStream_t>(stream));
+    l += launch_act_pack(dtype, x, ld_x, view, ctx->ws.status, ctx->shape, static_cast<cudaStream_t>(stream));
+  }
+  return leave(ctx);
+}
+
+qasg_status qasg_act_unpack(qasg_ctx* ctx, const qasg_act* act, qasg_dtype dtype, void* x, uint64_t ld_x,
+                            void* stream) {
+  ActView view;
+  qasg_status st = ctx ? check_act(act, &view) : QASG_ERR_INVALID_ARG;
+  if (st == QASG_OK) st = check_rows(dtype, x, ld_x, view.rows, view.cols);
+  if (st != QASG_OK || !view.rows) return st;
+  if ((st = enter(ctx)) != QASG_OK) return st;
+  {
+    Launch l(ctx, kActUnpack, static_cast<cudaStream_t>(stream));
+    l += launch_act_unpack(view, dtype, x, ld_x, ctx->shape, static_cast<cudaStream_t>(stream));
+  }
+  return leave(ctx);
+}
+
+uint64_t qasg_act_wgrad_scratch_bytes(uint64_t out_cols, uint64_t cols, uint32_t M) {
+  return act_wgrad_scratch_bytes(out_cols, cols, M);
+}
+
+qasg_status qasg_act_wgrad(qasg_ctx* ctx, qasg_dtype dtype, const void* dy, uint64_t ld_dy, uint64_t out_cols,
+                           const qasg_act* act, const float* weight, uint32_t M, const uint64_t* shard_row0, float* g,
+                           uint64_t ld_g, uint64_t ld_w, int accumulate, void* scratch, uint64_t scratch_bytes,
+                           void* stream) {
+  ActView view;
+  RowShards shards;
+  qasg_status st = ctx ? check_act(act, &view) : QASG_ERR_INVALID_ARG;
+  if (st == QASG_OK) st = check_rows(dtype, dy, ld_dy, view.rows, out_cols);
+  if (st == QASG_OK) st = check_row_shards(M, shard_row0, view.rows, &shards);
+  if (st != QASG_OK) return st;
+  if (out_cols < 1 || out_cols > kActMaxCols || !g || !scratch || ld_w < view.cols || ld_w > (1ull << 32))
+    return QASG_ERR_INVALID_ARG;
+  if (M > 1 && ld_g < (out_cols - 1) * ld_w + view.cols) return QASG_ERR_INVALID_ARG;
+  if (check_floats(g) != QASG_OK || check_floats(weight) != QASG_OK || !aligned16(scratch)) return QASG_ERR_ALIGNMENT;
+  if (scratch_bytes < act_wgrad_scratch_bytes(out_cols, view.cols, M)) return QASG_ERR_WORKSPACE;
+  if ((st = enter(ctx)) != QASG_OK) return st;
+  WgradArgs a;
+  a.dy = dy, a.weight = weight, a.g = g, a.scratch = scratch, a.scratch_bytes = scratch_bytes;
+  a.ld_dy = ld_dy, a.ld_g = ld_g, a.ld_w = ld_w, a.out_cols = static_cast<uint32_t>(out_cols), a.M = M;
+  a.accumulate = accumulate != 0;
+  {
+    Launch l(ctx, kActWgrad, static_cast<cudaStream_t>(stream));
+    l += launch_act_wgrad(dtype, a, view, shards, ctx->shape, static_cast<cudaStream_t>(stream));
+  }
+  return leave(ctx);
+}
+
+qasg_status qasg_rmsnorm_pack(qasg_ctx* ctx, qasg_dtype dtype, const void* x, uint64_t ld_x, const void* residual,
+                              uint64_t ld_r, const float* weight, float eps, void* h, uint64_t ld_h, void* y,
+                              uint64_t ld_y, const qasg_act* act, float* rstd, void* stream) {
+  ActView view;
+  qasg_status st = ctx ? check_act(act, &view) : QASG_ERR_INVALID_ARG;
+  if (st == QASG_OK) st = check_rows(dtype, x, ld_x, view.rows, view.cols);
+  if (st == QASG_OK && residual) st = check_rows(dtype, residual, ld_r, view.rows, view.cols);
+  if (st == QASG_OK && h) st = check_rows(dtype, h, ld_h, view.rows, view.cols);
+  if (st == QASG_OK && y) st = check_rows(dtype, y, ld_y, view.rows, view.cols);
+  if (st != QASG_OK) return st;
+  if (view.cols > kNormMaxCols || !(eps >= 0.f) || !isfinite(eps) || (!rstd && view.rows)) return QASG_ERR_INVALID_ARG;
+  if (check_floats(weight) != QASG_OK || check_floats(rstd) != QASG_OK) return QASG_ERR_ALIGNMENT;
+  if (!view.rows) return QASG_OK;
+  if ((st = enter(ctx)) != QASG_OK) return st;
+  NormArgs a;
+  a.x = x, a.residual = residual, a.weight = weight, a.h = h, a.y = y, a.rstd = rstd;
+  a.ld_x = ld_x, a.ld_r = ld_r, a.ld_h = ld_h, a.ld_y = ld_y, a.eps = eps;
+  {
+    Launch l(ctx, kRmsnormPack, static_cast<cudaStream_t>(stream));
+    l += launch_rmsnorm_pack(dtype, a, view, ctx->ws.status, ctx->shape, static_cast<cudaStream_t>(stream));
+  }
+  return leave(ctx);
+}
+
+uint64_t qasg_rmsnorm_grad_scratch_bytes(uint64_t cols, uint32_t M) { return rmsnorm_grad_scratch_bytes(cols, M); }
+
+qasg_status qasg_rmsnorm_grad(qasg_ctx* ctx, qasg_dtype dtype, const void* dy, uint64_t ld_dy, const void* dres,
+                              uint64_t ld_dres, const qasg_act* act, const float* rstd, const float* weight, uint32_t M,
+                              const uint64_t* shard_row0, void* dx, uint64_t ld_dx, float* gw, uint64_t ld_g,
+                              int accumulate, void* scratch, uint64_t scratch_bytes, void* stream) {
+  ActView view;
+  RowShards shards;
+  qasg_status st = ctx ? check_act(act, &view) : QASG_ERR_INVALID_ARG;
+  if (st == QASG_OK) st = check_rows(dtype, dy, ld_dy, view.rows, view.cols);
+  if (st == QASG_OK && dres) st = check_rows(dtype, dres, ld_dres, view.rows, view.cols);
+  if (st == QASG_OK) st = check_rows(dtype, dx, ld_dx, view.rows, view.cols);
+  if (st == QASG_OK) st = check_row_shards(M, shard_row0, view.rows, &shards);
+  if (st != QASG_OK) return st;
+  if (view.cols > kNormMaxCols || (!rstd && view.rows)) return QASG_ERR_INVALID_ARG;
+  if (gw && (!scratch || (M > 1 && ld_g < view.cols))) return QASG_ERR_INVALID_ARG;
+  if (check_floats(weight) != QASG_OK || check_floats(rstd) != QASG_OK || check_floats(gw) != QASG_OK || !aligned16(scratch))
+    return QASG_ERR_ALIGNMENT;
+  if (gw && scratch_bytes < rmsnorm_grad_scratch_bytes(view.cols, M)) return QASG_ERR_WORKSPACE;
+  if (!view.rows && !gw) return QASG_OK;
+  if ((st = enter(ctx)) != QASG_OK) return st;
+  NormGradArgs a;
+  a.dy = dy, a.dres = dres, a.rstd = rstd, a.weight = weight, a.dx = dx, a.gw = gw;
+  a.partials = static_cast<float*>(scratch);
+  a.ld_dy = ld_dy, a.ld_dres = ld_dres, a.ld_dx = ld_dx, a.ld_g = ld_g, a.M = M, a.accumulate = accumulate != 0;
+  {
+    Launch l(ctx, kRmsnormGrad, static_cast<cudaStream_t>(stream));
+    l += launch_rmsnorm_grad(dtype, a, view, shards, ctx->shape, static_cast<cudaStream_t>(stream));
+  }
+  return leave(ctx);
+}
+
+qasg_status qasg_token_logprob(qasg_ctx* ctx, qasg_dtype dtype, const void* logits, uint64_t ld, uint64_t rows,
+                               uint64_t vocab, const int64_t* tokens, float* logprob, float* entropy, float* lse,
+                               uint32_t k, int64_t* top_ids, float* top_logprob, void* stream) {
+  if (!ctx || vocab < 1 || vocab > kMaxRows || rows > kMaxRows / 8) return QASG_ERR_INVALID_ARG;
+  qasg_status st = check_rows(dtype, logits, ld, rows, vocab);
+  if (st != QASG_OK) return st;
+  if (k > kMaxTop || k > vocab || (logprob && !tokens)) return QASG_ERR_INVALID_ARG;
+  if (check_floats(logprob) != QASG_OK || check_floats(entropy) != QASG_OK || check_floats(lse) != QASG_OK ||
+      check_floats(top_logprob) != QASG_OK || (reinterpret_cast<uintptr_t>(tokens) & 7u) ||
+      (reinterpret_cast<uintptr_t>(top_ids) & 7u))
+    return QASG_ERR_ALIGNMENT;
+  if (!rows) return QASG_OK;
+  if ((st = enter(ctx)) != QASG_OK) return st;
+  LogprobArgs a;
+  a.logits = logits, a.tokens = tokens, a.logprob = logprob, a.entropy = entropy, a.lse = lse;
+  a.top_ids = top_ids, a.top_logprob = top_logprob, a.ld = ld, a.rows = rows;
+  a.vocab = static_cast<uint32_t>(vocab), a.k = top_ids || top_logprob ? k : 0u;
+  {
+    Launch l(ctx, kTokenLogprob, static_cast<cudaStream_t>(stream));
+    l += launch_token_logprob(dtype, a, ctx->ws.status, ctx->shape, static_cast<cudaStream_t>(stream));
+  }
+  return leave(ctx);
+}
+
+qasg_status qasg_token_logprob_grad(qasg_ctx* ctx, qasg_dtype dtype, const void* logits, uint64_t ld, uint64_t rows,
+                                    uint64_t vocab, const int64_t* tokens, const float* lse, const float* entropy,
+                                    const float* g_logprob, const float* g_entropy, const float* g_lse, void* dlogits,
+                                    uint64_t ld_d, void* stream) {
+  if (!ctx || vocab < 1 || vocab > kMaxRows || rows > kMaxRows) return QASG_ERR_INVALID_ARG;
+  qasg_status st = check_rows(dtype, logits, ld, rows, vocab);
+  if (st == QASG_OK) st = check_rows(dtype, dlogits, ld_d, rows, vocab);
+  if (st != QASG_OK) return st;
+  if (rows && (!lse || (g_entropy && !entropy))) return QASG_ERR_INVALID_ARG;
+  if (rows * (vocab / 8192 + 2) > kMaxRows) return QASG_ERR_INVALID_ARG;  // more work items than a launch holds
+  if (check_floats(lse) != QASG_OK || check_floats(entropy) != QASG_OK || check_floats(g_logprob) != QASG_OK ||
+      check_floats(g_entropy) != QASG_OK || check_floats(g_lse) != QASG_OK || (reinterpret_cast<uintptr_t>(tokens) & 7u))
+    return QASG_ERR_ALIGNMENT;
+  if (!rows) return QASG_OK;
+  if ((st = enter(ctx)) != QASG_OK) return st;
+  LogprobGradArgs a;
+  a.logits = logits, a.tokens = tokens, a.lse = lse, a.entropy = entropy, a.g_logprob = g_logprob;
+  a.g_entropy = g_entropy, a.g_lse = g_lse, a.dlogits = dlogits, a.ld = ld, a.ld_d = ld_d, a.rows = rows;
+  a.vocab = static_cast<uint32_t>(vocab);
+  {
+    Launch l(ctx, kTokenLogprobGrad, static_cast<cudaStream_t>(stream));
+    l += launch_token_logprob_grad(dtype, a, ctx->ws.status, ctx->shape, static_cast<cudaStream_t>(stream));
+  }
+  return leave(ctx);
+}
+
 qasg_status qasg_last_async_status(qasg_ctx* ctx, void* stream) {
   if (!ctx) return QASG_ERR_INVALID_ARG;
   if (enter(ctx) != QASG_OK) return QASG_ERR_CUDA;
@@ -872,7 +1073,8 @@ const char* qasg_kernel_name(int id) {
       "decode_average", "dense_update_cmd", "dense_update_rda", "logreg_dense", "logreg_csr", "avg_abs_sum",
       "avg_abs_max", "avg_threshold_codes", "avg_stochastic_codes", "select_stats", "indicator_or",
       "touched_clear", "logreg_csr_touched", "optimal_threshold", "mean_update_cmd", "mean_update_rda",
-      "quantize_stream_threshold", "quantize_stream_stochastic", "fused_step_cmd", "fused_step_rda"};
+      "quantize_stream_threshold", "quantize_stream_stochastic", "fused_step_cmd", "fused_step_rda",
+      "act_pack", "act_unpack", "act_wgrad", "rmsnorm_pack", "rmsnorm_grad", "token_logprob", "token_logprob_grad"};
   return (id >= 0 && id < kKernelIdCount) ? names[id] : "";
 }
 

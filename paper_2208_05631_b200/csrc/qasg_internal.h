@@ -191,5 +191,96 @@ int launch_fused_step(int rule, bool stochastic, const float* g, const Geometry&
 
 void query_launch_shape(LaunchShape* shape);
 
+// ------------------------------------------------------------------ language-model operators
+enum : int { kDtypeF32 = 0, kDtypeBf16 = 1, kDtypeF16 = 2 };  // the values of qasg_dtype
+
+// An 8-bit checkpoint on validated arguments: 1 <= cols <= 2^30, rows of whole blocks.
+struct ActView {
+  int8_t* codes;
+  uint8_t* exps;
+  uint64_t rows, ld_codes, ld_exps;
+  uint32_t cols;
+};
+
+int launch_act_pack(int dtype, const void* x, uint64_t ld_x, const ActView& act, unsigned int* status,
+                    const LaunchShape& shape, cudaStream_t stream);
+int launch_act_unpack(const ActView& act, int dtype, void* x, uint64_t ld_x, const LaunchShape& shape,
+                      cudaStream_t stream);
+
+// The rows of worker m are [row0[m], row0[m + 1]); any of these ranges may be empty.
+struct RowShards {
+  uint64_t row0[kMaxWorkers + 1];
+};
+
+struct NormArgs {
+  const void* x;
+  const void* residual;  // NULL: none
+  const float* weight;   // NULL: ones
+  void* h;               // NULL: not wanted
+  void* y;               // NULL: not wanted
+  float* rstd;
+  uint64_t ld_x, ld_r, ld_h, ld_y;
+  float eps;
+};
+int launch_rmsnorm_pack(int dtype, const NormArgs& a, const ActView& act, unsigned int* status, const LaunchShape& shape,
+                        cudaStream_t stream);
+
+struct NormGradArgs {
+  const void* dy;
+  const void* dres;     // NULL: none
+  const float* rstd;
+  const float* weight;  // NULL: ones
+  void* dx;
+  float* gw;            // NULL: not wanted; row m at gw + m * ld_g
+  float* partials;      // scratch
+  uint64_t ld_dy, ld_dres, ld_dx, ld_g;
+  uint32_t M;
+  bool accumulate;
+};
+constexpr uint32_t kNormMaxCols = 16384;
+uint64_t rmsnorm_grad_scratch_bytes(uint64_t cols, uint32_t M);
+int launch_rmsnorm_grad(int dtype, const NormGradArgs& a, const ActView& act, const RowShards& shards,
+                        const LaunchShape& shape, cudaStream_t stream);
+
+struct WgradArgs {
+  const void* dy;
+  const float* weight;  // NULL: ones; one factor per column of the checkpoint
+  float* g;             // worker m's gradient at g + m * ld_g, row n at + n * ld_w
+  void* scratch;
+  uint64_t scratch_bytes, ld_dy, ld_g, ld_w;
+  uint32_t out_cols, M;
+  bool accumulate;
+};
+uint64_t act_wgrad_scratch_bytes(uint64_t out_cols, uint64_t cols, uint32_t M);
+int launch_act_wgrad(int dtype, const WgradArgs& a, const ActView& act, const RowShards& shards, const LaunchShape& shape,
+                     cudaStream_t stream);
+
+constexpr uint32_t kMaxTop = 32;
+struct LogprobArgs {
+  const void* logits;
+  const int64_t* tokens;  // NULL: every row counts and no token is given
+  float* logprob;         // each output may be NULL
+  float* entropy;
+  float* lse;
+  int64_t* top_ids;
+  float* top_logprob;
+  uint64_t ld, rows;
+  uint32_t vocab, k;
+};
+int launch_token_logprob(int dtype, const LogprobArgs& a, unsigned int* status, const LaunchShape& shape,
+                         cudaStream_t stream);
+
+struct LogprobGradArgs {
+  const void* logits;
+  const int64_t* tokens;
+  const float *lse, *entropy;
+  const float *g_logprob, *g_entropy, *g_lse;  // each may be NULL: zeros
+  void* dlogits;
+  uint64_t ld, ld_d, rows;
+  uint32_t vocab;
+};
+int launch_token_logprob_grad(int dtype, const LogprobGradArgs& a, unsigned int* status, const LaunchShape& shape,
+                              cudaStream_t stream);
+
 }  // namespace qasg
 #endif  // QASG_INTERNAL_H_

@@ -1,0 +1,191 @@
+// Device-side building blocks shared by the language-model operators: element types, units of eight
+// values, the 8-bit block format, launches as programmatic dependents and in clusters.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "qasg_device.cuh"
+
+namespace qasg {
+
+constexpr int kUnit = 8;                          // values a thread moves at once
+constexpr int kActBlock = 32;                     // values that share one exponent byte: four units
+constexpr int kUnitsPerBlock = kActBlock / kUnit;
+
+// ------------------------------------------------------------------ element types
+__device__ __forceinline__ float to_float(float v) { return v; }
+__device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ float to_float(__half v) { return __half2float(v); }
+template <typename T> __device__ __forceinline__ T from_float(float v);
+template <> __device__ __forceinline__ float from_float<float>(float v) { return v; }
+template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+template <> __device__ __forceinline__ __half from_float<__half>(float v) { return __float2half_rn(v); }
+
+__device__ __forceinline__ float2 unpack2(uint32_t w, __nv_bfloat16) {
+  return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+}
+__device__ __forceinline__ float2 unpack2(uint32_t w, __half) {
+  return __half22float2(*reinterpret_cast<const __half2*>(&w));
+}
+__device__ __forceinline__ uint32_t pack2(float a, float b, __nv_bfloat16) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ uint32_t pack2(float a, float b, __half) {
+  const __half2 v = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+__device__ __forceinline__ bool is_aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+// The raw words of one unit: 4 for the 16-bit types, 8 for fp32.
+template <typename T> struct Unit { uint32_t w[kUnit * sizeof(T) / 4]; };
+
+// A unit on a 16-byte boundary; streaming (evict-first) where the data is read once and never again.
+template <typename T> __device__ __forceinline__ Unit<T> load_unit(const T* p) {
+  Unit<T> u;
+  const uint4* q = reinterpret_cast<const uint4*>(p);
+#pragma unroll
+  for (int i = 0; i < static_cast<int>(sizeof(u) / 16); ++i) {
+    const uint4 v = __ldcs(q + i);
+    u.w[4 * i] = v.x, u.w[4 * i + 1] = v.y, u.w[4 * i + 2] = v.z, u.w[4 * i + 3] = v.w;
+  }
+  return u;
+}
+template <typename T> __device__ __forceinline__ void unit_floats(const Unit<T>& u, float (&v)[kUnit]) {
+#pragma unroll
+  for (int i = 0; i < kUnit / 2; ++i) {
+    const float2 f = unpack2(u.w[i], T());
+    v[2 * i] = f.x, v[2 * i + 1] = f.y;
+  }
+}
+template <> __device__ __forceinline__ void unit_floats<float>(const Unit<float>& u, float (&v)[kUnit]) {
+#pragma unroll
+  for (int i = 0; i < kUnit; ++i) v[i] = __uint_as_float(u.w[i]);
+}
+
+// Values [i, i + 8) of a row of n values, `fill` outside the row; any alignment of the row.
+template <typename T>
+__device__ __forceinline__ void load_values(const T* row, int64_t i, int64_t n, float fill, float (&v)[kUnit]) {
+  if (i >= 0 && i + kUnit <= n && is_aligned16(row + i)) {
+    unit_floats(load_unit(row + i), v);
+  } else {
+#pragma unroll
+    for (int k = 0; k < kUnit; ++k) v[k] = (i + k >= 0 && i + k < n) ? to_float(row[i + k]) : fill;
+  }
+}
+
+template <typename T> __device__ __forceinline__ void store_unit(T* p, const float (&v)[kUnit]) {
+  uint4 q;
+  q.x = pack2(v[0], v[1], T()), q.y = pack2(v[2], v[3], T()), q.z = pack2(v[4], v[5], T()), q.w = pack2(v[6], v[7], T());
+  *reinterpret_cast<uint4*>(p) = q;
+}
+template <> __device__ __forceinline__ void store_unit<float>(float* p, const float (&v)[kUnit]) {
+  reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+  reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+}
+template <typename T>
+__device__ __forceinline__ void store_values(T* row, int64_t i, int64_t n, const float (&v)[kUnit]) {
+  if (i >= 0 && i + kUnit <= n && is_aligned16(row + i)) {
+    store_unit(row + i, v);
+  } else {
+#pragma unroll
+    for (int k = 0; k < kUnit; ++k)
+      if (i + k >= 0 && i + k < n) row[i + k] = from_float<T>(v[k]);
+  }
+}
+
+// ------------------------------------------------------------------ the 8-bit block format
+// A block of 32 values shares the byte b = E + 127, E = max(floor(log2 max|a|), -120): the exponent field of
+// the largest magnitude, at least 7, so that 2^(E-6) is a normal number.  A code is a * 2^(6-E) (exact)
+// rounded to the nearest integer, ties to even, within [-127, 127]: 7 significant bits, so code * 2^(E-6)
+// is exact in bf16 and fp32.  A block with an infinity or a NaN has b = 255 and stands for 32 NaNs.
+constexpr uint32_t kActNan = 255u;
+constexpr float kRoundMagic = 12582912.f;  // 1.5 * 2^23: adding it rounds to an integer in the low bits
+
+__device__ __forceinline__ uint32_t act_exponent(float largest) {  // largest >= 0, infinite or NaN
+  const uint32_t f = __float_as_uint(largest) >> 23;
+  return f < 7u ? 7u : f;
+}
+__device__ __forceinline__ float act_scale(uint32_t b) { return __uint_as_float((260u - b) << 23); }  // 2^(6-E)
+__device__ __forceinline__ float act_unit(uint32_t b) {                                              // 2^(E-6)
+  return b == kActNan ? __uint_as_float(0x7fffffffu) : __uint_as_float((b - 6u) << 23);
+}
+// Largest magnitude of a block held by four adjacent lanes, eight values each; NaN if any value is.
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float block_largest(const float (&v)[kUnit]) {
+  float m = 0.f;
+#pragma unroll
+  for (int i = 0; i < kUnit; ++i) m = max_nan(m, fabsf(v[i]));
+  m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, 1));
+  return max_nan(m, __shfl_xor_sync(0xffffffffu, m, 2));
+}
+// Codes of one unit as eight bytes; v becomes the rounded codes as floats (0 in a NaN block).
+__device__ __forceinline__ uint2 act_codes(float (&v)[kUnit], uint32_t b) {
+  uint32_t w[kUnit];
+  const bool bad = b == kActNan;
+  const float s = act_scale(b);
+#pragma unroll
+  for (int i = 0; i < kUnit; ++i) {
+    const float r = (bad ? 0.f : fminf(fmaxf(v[i] * s, -127.f), 127.f)) + kRoundMagic;
+    w[i] = __float_as_uint(r);
+    v[i] = r - kRoundMagic;
+  }
+  uint2 c;
+  c.x = __byte_perm(__byte_perm(w[0], w[1], 0x0040), __byte_perm(w[2], w[3], 0x0040), 0x5410);
+  c.y = __byte_perm(__byte_perm(w[4], w[5], 0x0040), __byte_perm(w[6], w[7], 0x0040), 0x5410);
+  return c;
+}
+// The codes of eight bytes as floats: byte + 128 under the exponent of 2^23, minus 2^23 + 128.
+__device__ __forceinline__ void code_floats(uint2 c, float (&v)[kUnit]) {
+  const uint32_t w[2] = {c.x ^ 0x80808080u, c.y ^ 0x80808080u};
+#pragma unroll
+  for (int i = 0; i < kUnit; ++i)
+    v[i] = __uint_as_float(__byte_perm(w[i >> 2], 0x4B000000u, 0x7440 + (i & 3))) - 8388736.f;
+}
+
+// ------------------------------------------------------------------ reductions
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+  for (int s = 16; s > 0; s >>= 1) v += __shfl_xor_sync(0xffffffffu, v, s);
+  return v;
+}
+
+// ------------------------------------------------------------------ launches
+// Calls f with a value of the element type (the dtype has been checked).
+template <typename F> inline void with_dtype(int dtype, F f) {
+  if (dtype == kDtypeBf16) f(__nv_bfloat16());
+  else if (dtype == kDtypeF16) f(__half());
+  else f(0.f);
+}
+
+template <typename... KArgs, typename... Args>
+inline cudaError_t launch_lm(void (*kernel)(KArgs...), dim3 grid, unsigned block, size_t smem, unsigned cluster,
+                             cudaStream_t stream, bool chained, Args... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(block);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[2];
+  unsigned n = 0;
+  if (chained) {
+    attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[n++].val.programmaticStreamSerializationAllowed = 1;
+  }
+  if (cluster > 1) {
+    attr[n].id = cudaLaunchAttributeClusterDimension;
+    attr[n].val.clusterDim.x = cluster;
+    attr[n].val.clusterDim.y = 1;
+    attr[n++].val.clusterDim.z = 1;
+  }
+  cfg.attrs = attr;
+  cfg.numAttrs = n;
+  return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
+}
+
+}  // namespace qasg

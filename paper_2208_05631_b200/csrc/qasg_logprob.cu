@@ -1,0 +1,338 @@
+// Log probabilities of given tokens with entropy and top alternatives, and their gradient.
+//   lse = log sum_v exp(x_v);  logprob = x_token - lse;  entropy = lse - sum_v p_v x_v,  p = exp(x - lse);
+//   dx_v = p_v (g_lse - g_logprob - g_entropy (log p_v + entropy)) + [v = token] g_logprob.
+// Forward: one pass over the logits.  A thread keeps the running maximum m, s = sum 2^y and t = sum y 2^y with
+// y = (x - m) log2(e); when m grows by d (in units of log2), s becomes 2^-d s and t becomes 2^-d (t - d s).
+// Alternatives: a candidate is an element at least as large as a lower bound of the k-th largest value seen so
+// far; candidates go to a short list in shared memory that is cut back to its k best, which raises the bound.
+// A row is shared by the CTAs of a cluster where there are fewer rows than the GPU has room for.
+#include <cooperative_groups.h>
+
+#include "qasg_lm.cuh"
+
+namespace qasg {
+namespace cg = cooperative_groups;
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kTiny = -160.f;  // 2^kTiny is 0 in fp32: stands for every smaller power, so that 0 * y is 0
+constexpr int kRowUnits = 4;     // units a thread loads per round
+constexpr int kListSize = 1024;  // candidates kept before they are cut back to the k best
+constexpr int kMaxCluster = 8;
+
+__device__ __forceinline__ float exp2_fast(float y) {
+  float r;
+  asm("ex2.approx.f32 %0, %1;" : "=f"(r) : "f"(y));
+  return r;
+}
+
+// Keys order values, NaN above all, then columns, the lowest first; the two zeros are equal.
+__device__ __forceinline__ uint32_t value_order(float x) {
+  if (x != x) return 0xffffffffu;
+  const uint32_t b = __float_as_uint(x + 0.f);
+  return b ^ ((b >> 31) ? 0xffffffffu : 0x80000000u);
+}
+__device__ __forceinline__ unsigned long long value_key(float x, uint32_t column) {
+  return (static_cast<unsigned long long>(value_order(x)) << 32) | (0xffffffffu - column);
+}
+__device__ __forceinline__ float key_value(unsigned long long key) {
+  const uint32_t o = static_cast<uint32_t>(key >> 32);
+  return __uint_as_float(o == 0xffffffffu ? 0x7fffffffu : (o >> 31) ? (o ^ 0x80000000u) : ~o);
+}
+
+struct RowSums {
+  float m, s, t;
+};
+// Adds o to a; either may be empty (m = -inf, s = t = 0).
+__device__ __forceinline__ RowSums join(RowSums a, RowSums o) {
+  const float m = max_nan(a.m, o.m), base = m == -INFINITY ? 0.f : m;
+  const float da = max_nan((a.m - base) * kLog2e, kTiny), db = max_nan((o.m - base) * kLog2e, kTiny);
+  const float ca = exp2_fast(da), cb = exp2_fast(db);
+  RowSums r;
+  r.m = m;
+  r.s = fmaf(ca, a.s, cb * o.s);
+  r.t = fmaf(ca, fmaf(a.s, da, a.t), cb * fmaf(o.s, db, o.t));
+  return r;
+}
+
+struct RowShared {
+  unsigned long long list[kListSize];
+  unsigned long long best[kMaxTop];
+  float group_max[32];
+  RowSums warp_sums[32];
+  RowSums sums;
+  unsigned int count;
+  unsigned long long bound;
+};
+
+// Cuts the list back to its k best, in order, also in `best`; raises the bound.  Called by all threads; what
+// they pushed before is seen.  Keys are distinct, so an element's rank is the number of larger ones.
+template <int kThreads>
+__device__ __forceinline__ void cut_list(RowShared& sh, uint32_t k) {
+  __syncthreads();
+  const uint32_t n = min(sh.count, static_cast<unsigned>(kListSize));
+  for (uint32_t i = threadIdx.x; i < n; i += kThreads) {
+    const unsigned long long key = sh.list[i];
+    uint32_t rank = 0;
+    for (uint32_t j = 0; j < n; ++j) rank += sh.list[j] > key;
+    if (rank < k) sh.best[rank] = key;
+  }
+  __syncthreads();
+  const uint32_t kept = min(n, k);
+  for (uint32_t i = threadIdx.x; i < kept; i += kThreads) sh.list[i] = sh.best[i];
+  if (threadIdx.x == 0) {
+    sh.count = kept;
+    if (kept == k) sh.bound = max(sh.bound, sh.best[k - 1] + 1ull);
+  }
+  __syncthreads();
+}
+
+template <typename T, int kThreads, bool kTop>
+__global__ void __launch_bounds__(kThreads)
+token_logprob_kernel(LogprobArgs a, uint32_t cluster, unsigned int* __restrict__ status) {
+  __shared__ RowShared sh;
+  const uint64_t row = blockIdx.x / cluster;
+  const uint32_t part = blockIdx.x - static_cast<uint32_t>(row) * cluster, tid = threadIdx.x, vocab = a.vocab;
+  chain_wait();
+  chain_trigger();
+  const T* x = static_cast<const T*>(a.logits) + row * a.ld;
+  int64_t token = 0;
+  if (a.tokens) {
+    token = a.tokens[row];
+    if (token < 0 || token >= vocab) {  // the whole cluster leaves: a padding row is not read
+      if (part == 0) {
+        if (tid == 0) {
+          if (a.logprob) a.logprob[row] = 0.f;
+          if (a.entropy) a.entropy[row] = 0.f;
+          if (a.lse) a.lse[row] = 0.f;
+          if (token >= vocab) atomicOr(status, kFlagBadIndex);
+        }
+        if (kTop && tid < a.k) {
+          if (a.top_ids) a.top_ids[row * a.k + tid] = -1;
+          if (a.top_logprob) a.top_logprob[row * a.k + tid] = 0.f;
+        }
+      }
+      return;
+    }
+  }
+  const float given = to_float(x[token]);
+  if (kTop) {
+    if (tid == 0) sh.count = 0, sh.bound = 0;
+    __syncthreads();
+  }
+  // units on 16-byte boundaries: unit u holds columns 8u - off .. 8u - off + 7
+  const uint32_t off = static_cast<uint32_t>((reinterpret_cast<uintptr_t>(x) & 15u) / sizeof(T));
+  const uint32_t units = (vocab + off + kUnit - 1) / kUnit, per_part = (units + cluster - 1) / cluster;
+  const uint32_t u0 = part * per_part, u1 = min(units, u0 + per_part);
+  RowSums r = {-INFINITY, 0.f, 0.f};
+  float base = 0.f;  // m, 0 while m is -inf
+  float bound = -INFINITY;
+  for (uint32_t u = u0; u < u1; u += kThreads * kRowUnits) {
+    float v[kRowUnits][kUnit], top[kRowUnits];
+#pragma unroll
+    for (int j = 0; j < kRowUnits; ++j) {
+      const uint32_t w = u + j * kThreads + tid;
+      load_values<T>(x, static_cast<int64_t>(w) * kUnit - off, w < u1 ? vocab : 0, -INFINITY, v[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < kRowUnits; ++j) {
+      top[j] = v[j][0];
+#pragma unroll
+      for (int k = 1; k < kUnit; ++k) top[j] = max_nan(top[j], v[j][k]);
+    }
+    const float m = max_nan(max_nan(top[0], top[1]), max_nan(top[2], top[3]));
+    if (!(m <= r.m)) {
+      const float d = max_nan((r.m - m) * kLog2e, kTiny), c = exp2_fast(d);
+      r.t = c * fmaf(r.s, d, r.t);
+      r.s *= c;
+      r.m = m;
+      base = m;
+    }
+#pragma unroll
+    for (int j = 0; j < kRowUnits; ++j)
+#pragma unroll
+      for (int k = 0; k < kUnit; ++k) {
+        const float y = max_nan((v[j][k] - base) * kLog2e, kTiny), e = exp2_fast(y);
+        r.s += e;
+        r.t = fmaf(e, y, r.t);
+      }
+    if (kTop) {
+      if (u == u0) {
+        // 32 groups of threads hold distinct elements: the smallest of the groups' largest is at most the
+        // 32nd largest element, so at most the k-th largest
+        constexpr int kLanes = kThreads / 32;
+        float g = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+#pragma unroll
+        for (int s = kLanes / 2; s > 0; s >>= 1) g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, s));
+        if (tid % kLanes == 0) sh.group_max[tid / kLanes] = g;
+        __syncthreads();
+        g = sh.group_max[tid & 31];
+#pragma unroll
+        for (int s = 16; s > 0; s >>= 1) g = fminf(g, __shfl_xor_sync(0xffffffffu, g, s));
+        bound = g;
+        if (tid == 0) sh.bound = static_cast<unsigned long long>(value_order(g)) << 32;
+        __syncthreads();
+      }
+      uint32_t pending = 0;  // elements the full list had no room for
+      bool crowded = false;
+#pragma unroll
+      for (int j = 0; j < kRowUnits; ++j) {
+        if (top[j] < bound) continue;
+        const unsigned long long limit = sh.bound;
+        const int64_t c0 = static_cast<int64_t>(u + j * kThreads + tid) * kUnit - off;
+#pragma unroll
+        for (int k = 0; k < kUnit; ++k) {
+          if (v[j][k] < bound || c0 + k < 0 || c0 + k >= vocab || u + j * kThreads + tid >= u1) continue;
+          const unsigned long long key = value_key(v[j][k], static_cast<uint32_t>(c0 + k));
+          if (key < limit) continue;
+          const uint32_t at = atomicAdd(&sh.count, 1u);
+          if (at < kListSize) sh.list[at] = key;
+          else pending |= 1u << (j * kUnit + k);
+          crowded |= at >= kListSize / 2;
+        }
+      }
+      if (__syncthreads_or(crowded) || u == u0) {
+        cut_list<kThreads>(sh, a.k);
+        while (__syncthreads_or(pending != 0)) {
+          const unsigned long long limit = sh.bound;
+          for (uint32_t left = pending; left;) {
+            const int b = __ffs(left) - 1;
+            left &= left - 1;
+            const uint32_t c = static_cast<uint32_t>(static_cast<int64_t>(u + (b >> 3) * kThreads + tid) * kUnit - off + (b & 7));
+            const unsigned long long key = value_key(to_float(x[c]), c);
+            if (key >= limit) {
+              const uint32_t at = atomicAdd(&sh.count, 1u);
+              if (at >= kListSize) continue;  // stays pending
+              sh.list[at] = key;
+            }
+            pending &= ~(1u << b);
+          }
+          cut_list<kThreads>(sh, a.k);
+        }
+        bound = key_value(sh.bound);
+        if (bound != bound) bound = INFINITY;  // k NaNs: nothing but another NaN passes
+      }
+    }
+  }
+  // join the threads, then the CTAs
+#pragma unroll
+  for (int s = 16; s > 0; s >>= 1) {
+    RowSums o;
+    o.m = __shfl_xor_sync(0xffffffffu, r.m, s);
+    o.s = __shfl_xor_sync(0xffffffffu, r.s, s);
+    o.t = __shfl_xor_sync(0xffffffffu, r.t, s);
+    r = join(r, o);
+  }
+  if ((tid & 31) == 0) sh.warp_sums[tid >> 5] = r;
+  if (kTop) cut_list<kThreads>(sh, a.k);
+  else __syncthreads();
+  r = sh.warp_sums[0];
+#pragma unroll
+  for (int i = 1; i < kThreads / 32; ++i) r = join(r, sh.warp_sums[i]);
+  if (cluster > 1) {
+    cg::cluster_group group = cg::this_cluster();
+    if (tid == 0) sh.sums = r;
+    group.sync();
+    if (part == 0) {
+      for (uint32_t o = 1; o < cluster; ++o) {
+        const RowShared* other = group.map_shared_rank(&sh, o);
+        r = join(r, other->sums);
+        if (kTop && tid < other->count) {
+          const uint32_t at = atomicAdd(&sh.count, 1u);
+          sh.list[at] = other->list[tid];
+        }
+      }
+    }
+    group.sync();  // the other CTAs' shared memory has been read
+    if (part) return;
+    if (kTop) cut_list<kThreads>(sh, a.k);
+  }
+  const float log_s = logf(r.s);
+  const bool empty = r.m == -INFINITY;  // every logit is -inf
+  if (tid == 0) {
+    if (a.logprob) a.logprob[row] = empty ? -INFINITY : (given - r.m) - log_s;
+    if (a.entropy) a.entropy[row] = empty ? 0.f : log_s - r.t * kLn2 / r.s;
+    if (a.lse) a.lse[row] = empty ? -INFINITY : r.m + log_s;
+    if (!(fabsf(r.s) < INFINITY)) atomicOr(status, kFlagNonFinite);
+  }
+  if (kTop && tid < a.k) {
+    const unsigned long long key = sh.best[tid];
+    if (a.top_ids) a.top_ids[row * a.k + tid] = 0xffffffffu - static_cast<uint32_t>(key);
+    if (a.top_logprob) a.top_logprob[row * a.k + tid] = empty ? -INFINITY : (key_value(key) - r.m) - log_s;
+  }
+}
+
+// ------------------------------------------------------------------ gradient
+constexpr int kGradThreads = 256;
+template <typename T>
+__global__ void __launch_bounds__(kGradThreads)
+token_logprob_grad_kernel(LogprobGradArgs a, uint32_t per_row, unsigned int* __restrict__ status) {
+  const uint64_t row = blockIdx.x / per_row;
+  const uint32_t part = blockIdx.x - static_cast<uint32_t>(row) * per_row, vocab = a.vocab;
+  chain_wait();
+  chain_trigger();
+  const T* x = static_cast<const T*>(a.logits) + row * a.ld;
+  T* dx = static_cast<T*>(a.dlogits) + row * a.ld_d;
+  int64_t token = a.tokens ? a.tokens[row] : -1;
+  const bool skip = a.tokens && (token < 0 || token >= vocab);
+  if (skip && token >= 0 && part == 0 && threadIdx.x == 0) atomicOr(status, kFlagBadIndex);
+  const float lse = a.lse[row], g_lp = a.g_logprob && a.tokens ? a.g_logprob[row] : 0.f;
+  const float g_h = a.g_entropy ? a.g_entropy[row] : 0.f, g_lse = a.g_lse ? a.g_lse[row] : 0.f;
+  const bool zero = skip || lse == -INFINITY;  // a padding row, or one whose logits are all -inf
+  // p (c0 - c1 y) with y = log2 p
+  const float c0 = g_lse - g_lp - (a.g_entropy ? g_h * a.entropy[row] : 0.f), c1 = g_h * kLn2;
+  const uint32_t off = static_cast<uint32_t>((reinterpret_cast<uintptr_t>(dx) & 15u) / sizeof(T));
+  const uint32_t u0 = part * (kGradThreads * kRowUnits) + threadIdx.x;
+  float v[kRowUnits][kUnit];
+  if (!zero) {
+#pragma unroll
+    for (int j = 0; j < kRowUnits; ++j)
+      load_values<T>(x, static_cast<int64_t>(u0 + j * kGradThreads) * kUnit - off, vocab, -INFINITY, v[j]);
+  }
+#pragma unroll
+  for (int j = 0; j < kRowUnits; ++j) {
+    const int64_t c = static_cast<int64_t>(u0 + j * kGradThreads) * kUnit - off;
+#pragma unroll
+    for (int k = 0; k < kUnit; ++k) {
+      if (zero) {
+        v[j][k] = 0.f;
+      } else {
+        const float y = max_nan((v[j][k] - lse) * kLog2e, kTiny);
+        v[j][k] = exp2_fast(y) * fmaf(-c1, y, c0);
+        if (c + k == token) v[j][k] += g_lp;
+      }
+    }
+    store_values<T>(dx, c, vocab, v[j]);
+  }
+}
+
+// ------------------------------------------------------------------ launchers
+int launch_token_logprob(int dtype, const LogprobArgs& a, unsigned int* status, const LaunchShape& shape,
+                         cudaStream_t stream) {
+  // Rows are split over a cluster until there are about two CTAs for every SM, as long as a CTA keeps a round.
+  const bool narrow = a.vocab <= 4096;
+  uint32_t cluster = 1;
+  if (!narrow)
+    while (cluster < kMaxCluster && a.rows * cluster < static_cast<uint64_t>(shape.sm_count) && a.vocab / cluster > 16384) cluster *= 2;
+  with_dtype(dtype, [&](auto t) {
+    using T = decltype(t);
+    const dim3 grid(static_cast<unsigned>(a.rows * cluster));
+    auto go = [&](auto kernel, unsigned threads) { launch_lm(kernel, grid, threads, 0, cluster, stream, shape.chained, a, cluster, status); };
+    if (narrow) a.k ? go(token_logprob_kernel<T, 128, true>, 128) : go(token_logprob_kernel<T, 128, false>, 128);
+    else a.k ? go(token_logprob_kernel<T, 512, true>, 512) : go(token_logprob_kernel<T, 512, false>, 512);
+  });
+  return 1;
+}
+
+int launch_token_logprob_grad(int dtype, const LogprobGradArgs& a, unsigned int* status, const LaunchShape& shape,
+                              cudaStream_t stream) {
+  // one unit more than the row's: it may begin inside a 16-byte group
+  const uint32_t per_row = (a.vocab / kUnit + 2 + kGradThreads * kRowUnits - 1) / (kGradThreads * kRowUnits);
+  with_dtype(dtype, [&](auto t) {
+    using T = decltype(t);
+    launch_lm(token_logprob_grad_kernel<T>, dim3(static_cast<unsigned>(a.rows * per_row)), kGradThreads, 0, 1, stream,
+              shape.chained, a, per_row, status);
+  });
+  return 1;
+}
+
+}  // namespace qasg

@@ -1,0 +1,295 @@
+// Root-mean-square norm with the residual's addition and an output in 8 bits, and its gradient taken from
+// those 8 bits.
+//   h = x + residual;  rstd = 1 / sqrt(mean(h^2) + eps);  n = h * rstd;  n^ = what the 8-bit codes of n stand for;
+//   y = weight * n^.
+//   u = weight * dy;  dx = dres + rstd * (u - n^ * mean(u * n^));  dweight = sum over the rows of dy * n^.
+// Both are bound by HBM: a row is read once and kept in registers between its sum and its outputs.  kRowThreads
+// threads share a row, a thread owns kUnits units of eight adjacent columns, kRowThreads units apart.
+#include "qasg_lm.cuh"
+
+namespace qasg {
+
+// Threads of a CTA: a row's, or eight rows of a warp each.
+template <int kRowThreads> constexpr int kNormThreads = kRowThreads == 32 ? 256 : kRowThreads;
+
+// Sum over the threads of a row, the same bits in each of them.
+template <int kRowThreads>
+__device__ __forceinline__ float row_sum(float v, float* sm) {
+  v = warp_sum(v);
+  if (kRowThreads == 32) return v;
+  constexpr int kWarps = kRowThreads / 32;
+  if ((threadIdx.x & 31) == 0) sm[threadIdx.x >> 5] = v;
+  __syncthreads();
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < kWarps; ++i) s += sm[i];
+  return s;
+}
+
+__device__ __forceinline__ void load_weights(const float* __restrict__ weight, uint32_t c, uint32_t cols, float (&w)[kUnit]) {
+  if (c + kUnit <= cols && is_aligned16(weight + c)) {
+    const float4 a = load_f4(weight + c), b = load_f4(weight + c + 4);
+    w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w, w[4] = b.x, w[5] = b.y, w[6] = b.z, w[7] = b.w;
+  } else {
+#pragma unroll
+    for (int k = 0; k < kUnit; ++k) w[k] = c + k < cols ? __ldg(weight + c + k) : 0.f;
+  }
+}
+
+template <typename T, int kRowThreads, int kUnits>
+__global__ void __launch_bounds__(kNormThreads<kRowThreads>)
+rmsnorm_pack_kernel(NormArgs a, ActView act, unsigned int* __restrict__ status) {
+  constexpr int kRows = kNormThreads<kRowThreads> / kRowThreads;
+  __shared__ float sm[32];
+  const uint64_t row = static_cast<uint64_t>(blockIdx.x) * kRows + threadIdx.x / kRowThreads;
+  const uint32_t t = threadIdx.x % kRowThreads, cols = act.cols;
+  chain_wait();
+  chain_trigger();
+  if (kRows > 1 && row >= act.rows) return;  // whole warps: nothing meets below when a row is one warp
+  const T* x = static_cast<const T*>(a.x) + row * a.ld_x;
+  float v[kUnits][kUnit];
+#pragma unroll
+  for (int j = 0; j < kUnits; ++j) load_values<T>(x, (j * kRowThreads + t) * kUnit, cols, 0.f, v[j]);
+  if (a.residual) {
+    const T* r = static_cast<const T*>(a.residual) + row * a.ld_r;
+    float w[kUnits][kUnit];
+#pragma unroll
+    for (int j = 0; j < kUnits; ++j) load_values<T>(r, (j * kRowThreads + t) * kUnit, cols, 0.f, w[j]);
+#pragma unroll
+    for (int j = 0; j < kUnits; ++j)
+#pragma unroll
+      for (int k = 0; k < kUnit; ++k) v[j][k] += w[j][k];
+  }
+  float sq = 0.f;
+#pragma unroll
+  for (int j = 0; j < kUnits; ++j)
+#pragma unroll
+    for (int k = 0; k < kUnit; ++k) sq = fmaf(v[j][k], v[j][k], sq);
+  if (a.h) {
+    T* h = static_cast<T*>(a.h) + row * a.ld_h;
+#pragma unroll
+    for (int j = 0; j < kUnits; ++j) store_values<T>(h, (j * kRowThreads + t) * kUnit, cols, v[j]);
+  }
+  const float rstd = 1.f / sqrtf(row_sum<kRowThreads>(sq, sm) / static_cast<float>(cols) + a.eps);
+  if (t == 0) a.rstd[row] = rstd;
+  const uint32_t padded = (cols + kActBlock - 1) & ~static_cast<uint32_t>(kActBlock - 1);
+  bool bad = false;
+#pragma unroll
+  for (int j = 0; j < kUnits; ++j) {
+    const uint32_t c = (j * kRowThreads + t) * kUnit;
+#pragma unroll
+    for (int k = 0; k < kUnit; ++k) v[j][k] *= rstd;
+    const uint32_t b = act_exponent(block_largest(v[j]));
+    const uint2 codes = act_codes(v[j], b);
+    if (c >= padded) continue;
+    *reinterpret_cast<uint2*>(act.codes + row * act.ld_codes + c) = codes;
+    if ((t & 3) == 0) act.exps[row * act.ld_exps + c / kActBlock] = static_cast<uint8_t>(b);
+    bad |= b == kActNan;
+    if (!a.y) continue;
+    const float unit = act_unit(b);
+    if (a.weight) {
+      float w[kUnit];
+      load_weights(a.weight, c, cols, w);
+#pragma unroll
+      for (int k = 0; k < kUnit; ++k) v[j][k] = v[j][k] * unit * w[k];
+    } else {
+#pragma unroll
+      for (int k = 0; k < kUnit; ++k) v[j][k] *= unit;
+    }
+    store_values<T>(static_cast<T*>(a.y) + row * a.ld_y, c, cols, v[j]);
+  }
+  if (bad) atomicOr(status, kFlagNonFinite);
+}
+
+// ------------------------------------------------------------------ gradient
+// A CTA takes a run of rows of one worker and keeps their part of the weight gradient in registers; the runs'
+// parts are then added in order by a second launch, so the result does not depend on timing.
+struct NormRuns {
+  RowShards shards;
+  uint32_t run0[kMaxWorkers + 1];  // first run of each worker
+  uint32_t rows_per_run;
+};
+
+template <typename T, int kRowThreads, int kUnits>
+__global__ void __launch_bounds__(kNormThreads<kRowThreads>)
+rmsnorm_grad_kernel(NormGradArgs a, ActView act, const __grid_constant__ NormRuns runs) {
+  constexpr int kRows = kNormThreads<kRowThreads> / kRowThreads;
+  constexpr int kCols = kRowThreads * kUnits * kUnit;
+  __shared__ float sm[2][32];
+  __shared__ float sm_dw[kRows > 1 ? kRows : 1][kRows > 1 ? kCols : 1];
+  const uint32_t t = threadIdx.x % kRowThreads, cols = act.cols, sub = threadIdx.x / kRowThreads;
+  uint32_t m = 0;
+  while (m + 1 < a.M && runs.run0[m + 1] <= blockIdx.x) ++m;
+  const uint64_t first = runs.shards.row0[m] + static_cast<uint64_t>(blockIdx.x - runs.run0[m]) * runs.rows_per_run;
+  const uint64_t last = min(first + runs.rows_per_run, runs.shards.row0[m + 1]);
+  const uint32_t padded = (cols + kActBlock - 1) & ~static_cast<uint32_t>(kActBlock - 1);
+  chain_wait();
+  chain_trigger();
+  float w[kUnits][kUnit], dw[kUnits][kUnit];
+#pragma unroll
+  for (int j = 0; j < kUnits; ++j) {
+    if (a.weight) load_weights(a.weight, (j * kRowThreads + t) * kUnit, cols, w[j]);
+#pragma unroll
+    for (int k = 0; k < kUnit; ++k) {
+      if (!a.weight) w[j][k] = 1.f;
+      dw[j][k] = 0.f;
+    }
+  }
+  int turn = 0;
+  for (uint64_t row = first + sub; row < last; row += kRows, turn ^= 1) {
+    const T* dy = static_cast<const T*>(a.dy) + row * a.ld_dy;
+    float n[kUnits][kUnit], u[kUnits][kUnit];
+    float dot = 0.f;
+#pragma unroll
+    for (int j = 0; j < kUnits; ++j) {
+      const uint32_t c = (j * kRowThreads + t) * kUnit;
+      load_values<T>(dy, c, cols, 0.f, u[j]);
+      uint2 codes = make_uint2(0u, 0u);
+      uint32_t b = 7u;
+      if (c < padded) {
+        codes = __ldcs(reinterpret_cast<const uint2*>(act.codes + row * act.ld_codes + c));
+        b = act.exps[row * act.ld_exps + c / kActBlock];
+      }
+      code_floats(codes, n[j]);
+      const float unit = act_unit(b);
+#pragma unroll
+      for (int k = 0; k < kUnit; ++k) n[j][k] *= unit;
+    }
+#pragma unroll
+    for (int j = 0; j < kUnits; ++j)
+#pragma unroll
+      for (int k = 0; k < kUnit; ++k) {
+        dw[j][k] = fmaf(u[j][k], n[j][k], dw[j][k]);
+        u[j][k] *= w[j][k];
+        dot = fmaf(u[j][k], n[j][k], dot);
+      }
+    const float mean = row_sum<kRowThreads>(dot, sm[turn]) / static_cast<float>(cols), rstd = a.rstd[row];
+#pragma unroll
+    for (int j = 0; j < kUnits; ++j) {
+      const uint32_t c = (j * kRowThreads + t) * kUnit;
+      if (c >= cols) continue;
+#pragma unroll
+      for (int k = 0; k < kUnit; ++k) u[j][k] = rstd * fmaf(-n[j][k], mean, u[j][k]);
+      if (a.dres) {
+        float r[kUnit];
+        load_values<T>(static_cast<const T*>(a.dres) + row * a.ld_dres, c, cols, 0.f, r);
+#pragma unroll
+        for (int k = 0; k < kUnit; ++k) u[j][k] += r[k];
+      }
+      store_values<T>(static_cast<T*>(a.dx) + row * a.ld_dx, c, cols, u[j]);
+    }
+  }
+  if (!a.gw) return;
+  float* part = a.partials + static_cast<uint64_t>(blockIdx.x) * ((cols + 7u) & ~7u);
+  if (kRows > 1) {
+#pragma unroll
+    for (int j = 0; j < kUnits; ++j)
+#pragma unroll
+      for (int k = 0; k < kUnit; ++k) sm_dw[sub][(j * kRowThreads + t) * kUnit + k] = dw[j][k];
+    __syncthreads();
+    for (uint32_t c = threadIdx.x; c < cols; c += kNormThreads<kRowThreads>) {
+      float s = 0.f;
+#pragma unroll
+      for (int i = 0; i < kRows; ++i) s += sm_dw[i][c];
+      part[c] = s;
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < kUnits; ++j) {
+      const uint32_t c = (j * kRowThreads + t) * kUnit;
+      if (c < cols) store_unit<float>(part + c, dw[j]);  // rows of partials are whole units
+    }
+  }
+}
+
+// grid (columns / 32, workers): 32 columns of a worker, its runs dealt to kSumLanes lanes and those added in order.
+constexpr int kSumLanes = 16;
+__global__ void __launch_bounds__(32 * kSumLanes)
+run_sum_kernel(const float* __restrict__ partials, const __grid_constant__ NormRuns runs, uint32_t cols, float* __restrict__ gw,
+               uint64_t ld_g, bool accumulate) {
+  __shared__ float sm[kSumLanes][33];
+  const uint32_t lane = threadIdx.x & 31, slice = threadIdx.x >> 5, m = blockIdx.y;
+  const uint32_t c = blockIdx.x * 32 + lane, ld = (cols + 7u) & ~7u;
+  chain_wait();
+  chain_trigger();
+  float s = 0.f;
+  if (c < cols)
+#pragma unroll 4
+    for (uint32_t r = runs.run0[m] + slice; r < runs.run0[m + 1]; r += kSumLanes)
+      s += __ldcg(partials + static_cast<uint64_t>(r) * ld + c);
+  sm[slice][lane] = s;
+  __syncthreads();
+  if (slice || c >= cols) return;
+#pragma unroll
+  for (int i = 1; i < kSumLanes; ++i) s += sm[i][lane];
+  float* out = gw + m * ld_g + c;
+  *out = accumulate ? *out + s : s;
+}
+
+// ------------------------------------------------------------------ launchers
+// f(kRowThreads, kUnits) for a row of `cols` columns: the fewest threads that hold the row in at most four units
+// each.
+template <typename F> static void with_row(uint32_t cols, F f) {
+  using std::integral_constant;
+  if (cols <= 256) f(integral_constant<int, 32>(), integral_constant<int, 1>());
+  else if (cols <= 1024) f(integral_constant<int, 32>(), integral_constant<int, 4>());
+  else if (cols <= 2048) f(integral_constant<int, 128>(), integral_constant<int, 2>());
+  else if (cols <= 4096) f(integral_constant<int, 256>(), integral_constant<int, 2>());
+  else if (cols <= 8192) f(integral_constant<int, 512>(), integral_constant<int, 2>());
+  else f(integral_constant<int, 512>(), integral_constant<int, 4>());  // up to kNormMaxCols
+}
+
+int launch_rmsnorm_pack(int dtype, const NormArgs& a, const ActView& act, unsigned int* status, const LaunchShape& shape,
+                        cudaStream_t stream) {
+  with_dtype(dtype, [&](auto t) {
+    using T = decltype(t);
+    with_row(act.cols, [&](auto row_threads, auto units) {
+      constexpr int kThreadsRow = decltype(row_threads)::value;
+      constexpr unsigned kRows = kNormThreads<kThreadsRow> / kThreadsRow;
+      launch_lm(rmsnorm_pack_kernel<T, kThreadsRow, decltype(units)::value>,
+                dim3(static_cast<unsigned>((act.rows + kRows - 1) / kRows)), kNormThreads<kThreadsRow>, 0, 1, stream,
+                shape.chained, a, act, status);
+    });
+  });
+  return 1;
+}
+
+// Runs of rows: about one per resident CTA, at most kNormRuns, plus what the workers' ends add.
+constexpr uint32_t kNormRuns = 592, kNormRunsWide = 296;  // rows of up to 4096 columns, wider ones
+static uint32_t norm_runs(uint32_t cols) { return cols <= 4096 ? kNormRuns : kNormRunsWide; }
+uint64_t rmsnorm_grad_scratch_bytes(uint64_t cols, uint32_t M) {
+  return (norm_runs(static_cast<uint32_t>(cols)) + M) * ((cols + 7) & ~7ull) * sizeof(float);
+}
+
+int launch_rmsnorm_grad(int dtype, const NormGradArgs& a, const ActView& act, const RowShards& shards,
+                        const LaunchShape& shape, cudaStream_t stream) {
+  NormRuns runs;
+  runs.shards = shards;
+  const uint64_t rows = shards.row0[a.M] - shards.row0[0], most = norm_runs(act.cols);
+  runs.rows_per_run = static_cast<uint32_t>((rows + most - 1) / most);
+  if (act.cols <= 1024) runs.rows_per_run = (runs.rows_per_run + 7) / 8 * 8;  // eight rows at a time
+  if (!runs.rows_per_run) runs.rows_per_run = 1;
+  runs.run0[0] = 0;
+  for (uint32_t m = 0; m < a.M; ++m)
+    runs.run0[m + 1] = runs.run0[m] + static_cast<uint32_t>((shards.row0[m + 1] - shards.row0[m] + runs.rows_per_run - 1) / runs.rows_per_run);
+  int launches = 0;
+  if (runs.run0[a.M]) {
+    with_dtype(dtype, [&](auto t) {
+      using T = decltype(t);
+      with_row(act.cols, [&](auto row_threads, auto units) {
+        constexpr int kThreadsRow = decltype(row_threads)::value;
+        launch_lm(rmsnorm_grad_kernel<T, kThreadsRow, decltype(units)::value>, dim3(runs.run0[a.M]),
+                  kNormThreads<kThreadsRow>, 0, 1, stream, shape.chained, a, act, runs);
+      });
+    });
+    ++launches;
+  }
+  if (a.gw) {
+    launch_lm(run_sum_kernel, dim3((act.cols + 31) / 32, a.M), 32 * kSumLanes, 0, 1, stream, shape.chained, a.partials, runs,
+              act.cols, a.gw, a.ld_g, a.accumulate);
+    ++launches;
+  }
+  return launches;
+}
+
+}  // namespace qasg

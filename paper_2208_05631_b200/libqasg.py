@@ -23,6 +23,9 @@ CREATE_NO_CODE_SCRATCH = 1
 CREATE_SERIAL_LAUNCHES = 2
 OPT_STREAM_ROW_BYTES, OPT_STREAM_LAG, OPT_WAIT_POLLS, OPT_ONE_LAUNCH_STEP_BYTES = 0, 1, 2, 3
 LAG_AUTO = 0xFFFFFFFF
+F32, BF16, F16 = 0, 1, 2
+ACT_BLOCK = 32
+TOP_MAX = 32
 
 # Names every build of the library must export (checked by the CPU tests).
 EXPORTS = [
@@ -33,9 +36,11 @@ EXPORTS = [
     "qasg_select_quantize_pack", "qasg_indicator_or", "qasg_step_select",
     "qasg_logreg_grad_csr_touched", "qasg_quantize_pack_touched", "qasg_step_touched",
     "qasg_optimal_scratch_bytes", "qasg_quantize_pack_optimal", "qasg_set_option", "qasg_wait_selftest",
+    "qasg_act_pack", "qasg_act_unpack", "qasg_act_wgrad_scratch_bytes", "qasg_act_wgrad", "qasg_rmsnorm_pack",
+    "qasg_rmsnorm_grad_scratch_bytes", "qasg_rmsnorm_grad", "qasg_token_logprob", "qasg_token_logprob_grad",
 ]
 STATIC_MAX_WORKERS = 16
-KERNEL_COUNT = 26
+KERNEL_COUNT = 33
 
 
 class QasgError(RuntimeError):
@@ -48,6 +53,34 @@ class Params(ctypes.Structure):
     _fields_ = [("struct_size", ctypes.c_uint32), ("quantizer", ctypes.c_uint32),
                 ("thr_coef", ctypes.c_float), ("lambda_", ctypes.c_float), ("eta", ctypes.c_float),
                 ("delta", ctypes.c_float), ("seed", ctypes.c_uint64)]
+
+
+class _ActStruct(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("cols", ctypes.c_uint32), ("rows", ctypes.c_uint64),
+                ("codes", ctypes.c_void_p), ("exps", ctypes.c_void_p), ("ld_codes", ctypes.c_uint64),
+                ("ld_exps", ctypes.c_uint64)]
+
+
+class Act:
+    """A qasg_act over two tensors: codes int8 [rows][ld_codes] and exps uint8 [rows][ld_exps] (strides are
+    taken from the tensors), which it keeps alive."""
+
+    def __init__(self, codes, exps, rows, cols):
+        self.codes, self.exps, self.rows, self.cols = codes, exps, int(rows), int(cols)
+        self.struct = _ActStruct(ctypes.sizeof(_ActStruct), self.cols, self.rows, codes.data_ptr(), exps.data_ptr(),
+                                 codes.stride(0), exps.stride(0))
+        self.ref = ctypes.byref(self.struct)
+
+
+def new_act(rows, cols, device="cuda"):
+    """An Act over new tensors with the smallest leading dimensions that qasg_act allows."""
+    blocks = -(-cols // ACT_BLOCK)
+    return Act(torch.empty((rows, blocks * ACT_BLOCK), dtype=torch.int8, device=device),
+               torch.empty((rows, -(-blocks // 16) * 16), dtype=torch.uint8, device=device), rows, cols)
+
+
+def new_scratch(nbytes, device="cuda"):
+    return torch.empty(int(nbytes), dtype=torch.uint8, device=device)
 
 
 def make_params(lam=1e-3, eta=0.1, delta=1e-8, quantizer=Q_THRESHOLD, thr_coef=0.75, seed=0):
@@ -96,6 +129,19 @@ def load():
     lib.qasg_optimal_scratch_bytes.argtypes = [u64]
     lib.qasg_optimal_scratch_bytes.restype = u64
     lib.qasg_quantize_pack_optimal.argtypes = [vp, vp, u64, u64, u32, pp, vp, vp, vp, vp, vp, u64, vp]
+    lib.qasg_act_pack.argtypes = [vp, i32, vp, u64, vp, vp]
+    lib.qasg_act_unpack.argtypes = [vp, vp, i32, vp, u64, vp]
+    lib.qasg_act_wgrad_scratch_bytes.argtypes = [u64, u64, u32]
+    lib.qasg_act_wgrad_scratch_bytes.restype = u64
+    lib.qasg_act_wgrad.argtypes = [vp, i32, vp, u64, u64, vp, vp, u32, ctypes.POINTER(u64), vp, u64, u64, i32, vp, u64,
+                                   vp]
+    lib.qasg_rmsnorm_pack.argtypes = [vp, i32, vp, u64, vp, u64, vp, ctypes.c_float, vp, u64, vp, u64, vp, vp, vp]
+    lib.qasg_rmsnorm_grad_scratch_bytes.argtypes = [u64, u32]
+    lib.qasg_rmsnorm_grad_scratch_bytes.restype = u64
+    lib.qasg_rmsnorm_grad.argtypes = [vp, i32, vp, u64, vp, u64, vp, vp, vp, u32, ctypes.POINTER(u64), vp, u64, vp, u64,
+                                      i32, vp, u64, vp]
+    lib.qasg_token_logprob.argtypes = [vp, i32, vp, u64, u64, u64, vp, vp, vp, vp, u32, vp, vp, vp]
+    lib.qasg_token_logprob_grad.argtypes = [vp, i32, vp, u64, u64, u64, vp, vp, vp, vp, vp, vp, vp, u64, vp]
     lib.qasg_set_option.argtypes = [vp, i32, u64]
     lib.qasg_wait_selftest.argtypes = [vp, u32, vp]
     lib.qasg_last_async_status.argtypes = [vp, vp]
@@ -258,6 +304,44 @@ class Context:
                                                  scratch.numel() * scratch.element_size(), _stream(stream)),
                "qasg_quantize_pack_optimal")
 
+    # Language-model operators.  Where the C entry point takes a scratch pointer and its size, the methods take
+    # one tensor (new_scratch(..._scratch_bytes(...))).
+    def act_pack(self, dtype, x, ld_x, act, stream=None):
+        _check(load().qasg_act_pack(self._h, dtype, _ptr(x), ld_x, act.ref, _stream(stream)), "qasg_act_pack")
+
+    def act_unpack(self, act, dtype, x, ld_x, stream=None):
+        _check(load().qasg_act_unpack(self._h, act.ref, dtype, _ptr(x), ld_x, _stream(stream)), "qasg_act_unpack")
+
+    def act_wgrad(self, dtype, dy, ld_dy, out_cols, act, weight, M, shard_row0, g, ld_g, ld_w, accumulate, scratch,
+                  stream=None):
+        _check(load().qasg_act_wgrad(self._h, dtype, _ptr(dy), ld_dy, out_cols, act.ref, _ptr(weight), M,
+                                     _shards(shard_row0), _ptr(g), ld_g, ld_w, int(accumulate), _ptr(scratch),
+                                     scratch.numel() * scratch.element_size(), _stream(stream)), "qasg_act_wgrad")
+
+    def rmsnorm_pack(self, dtype, x, ld_x, residual, ld_r, weight, eps, h, ld_h, y, ld_y, act, rstd, stream=None):
+        _check(load().qasg_rmsnorm_pack(self._h, dtype, _ptr(x), ld_x, _ptr(residual), ld_r, _ptr(weight), eps, _ptr(h),
+                                        ld_h, _ptr(y), ld_y, act.ref, _ptr(rstd), _stream(stream)), "qasg_rmsnorm_pack")
+
+    def rmsnorm_grad(self, dtype, dy, ld_dy, dres, ld_dres, act, rstd, weight, M, shard_row0, dx, ld_dx, gw, ld_g,
+                     accumulate, scratch, stream=None):
+        _check(load().qasg_rmsnorm_grad(self._h, dtype, _ptr(dy), ld_dy, _ptr(dres), ld_dres, act.ref, _ptr(rstd),
+                                        _ptr(weight), M, _shards(shard_row0), _ptr(dx), ld_dx, _ptr(gw), ld_g,
+                                        int(accumulate), _ptr(scratch),
+                                        scratch.numel() * scratch.element_size() if scratch is not None else 0,
+                                        _stream(stream)), "qasg_rmsnorm_grad")
+
+    def token_logprob(self, dtype, logits, ld, rows, vocab, tokens, logprob, entropy, lse, k=0, top_ids=None,
+                      top_logprob=None, stream=None):
+        _check(load().qasg_token_logprob(self._h, dtype, _ptr(logits), ld, rows, vocab, _ptr(tokens), _ptr(logprob),
+                                         _ptr(entropy), _ptr(lse), k, _ptr(top_ids), _ptr(top_logprob),
+                                         _stream(stream)), "qasg_token_logprob")
+
+    def token_logprob_grad(self, dtype, logits, ld, rows, vocab, tokens, lse, entropy, g_logprob, g_entropy, g_lse,
+                           dlogits, ld_d, stream=None):
+        _check(load().qasg_token_logprob_grad(self._h, dtype, _ptr(logits), ld, rows, vocab, _ptr(tokens), _ptr(lse),
+                                              _ptr(entropy), _ptr(g_logprob), _ptr(g_entropy), _ptr(g_lse),
+                                              _ptr(dlogits), ld_d, _stream(stream)), "qasg_token_logprob_grad")
+
     def set_option(self, option, value):
         _check(load().qasg_set_option(self._h, int(option), int(value)), "qasg_set_option")
 
@@ -280,6 +364,14 @@ class Context:
 
     def launch_count(self):
         return int(load().qasg_launch_count(self._h))
+
+
+def act_wgrad_scratch_bytes(out_cols, cols, M):
+    return int(load().qasg_act_wgrad_scratch_bytes(int(out_cols), int(cols), int(M)))
+
+
+def rmsnorm_grad_scratch_bytes(cols, M):
+    return int(load().qasg_rmsnorm_grad_scratch_bytes(int(cols), int(M)))
 
 
 def optimal_scratch_bytes(d):
