@@ -902,7 +902,12 @@ qasg_status qasg_act_wgrad(qasg_ctx* ctx, qasg_dtype dtype, const void* dy, uint
   a.accumulate = accumulate != 0;
   {
     Launch l(ctx, kActWgrad, static_cast<cudaStream_t>(stream));
-    l += launch_act_wgrad(dtype, a, view, shards, ctx->shape, static_cast<cudaStream_t>(stream));
+    const int launched = launch_act_wgrad(dtype, a, view, shards, ctx->ws.status, ctx->shape, static_cast<cudaStream_t>(stream));
+    if (launched < 0) {
+      cudaGetLastError();
+      return QASG_ERR_CUDA;
+    }
+    l += launched;
   }
   return leave(ctx);
 }

@@ -252,8 +252,9 @@ struct WgradArgs {
   bool accumulate;
 };
 uint64_t act_wgrad_scratch_bytes(uint64_t out_cols, uint64_t cols, uint32_t M);
-int launch_act_wgrad(int dtype, const WgradArgs& a, const ActView& act, const RowShards& shards, const LaunchShape& shape,
-                     cudaStream_t stream);
+// -1: a tensor map or the launch configuration was refused
+int launch_act_wgrad(int dtype, const WgradArgs& a, const ActView& act, const RowShards& shards, unsigned int* status,
+                     const LaunchShape& shape, cudaStream_t stream);
 
 constexpr uint32_t kMaxTop = 32;
 struct LogprobArgs {

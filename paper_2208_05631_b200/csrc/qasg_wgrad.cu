@@ -1,59 +1,677 @@
 // Weight gradient of a linear layer from an 8-bit checkpoint of its input:
 //   g_m[n][k] (+)= weight_k * sum over the rows t of worker m of dy[t][n] * a^[t][k].
+//
+// A matrix product on the tensor cores (tcgen05, fp32 accumulators in tensor memory).  a^ = code * 2^(E-6) has 7
+// significant bits, so it is exact in bf16; dy in bf16 is taken as it is, fp16 as the sum of two bf16 pieces and
+// fp32 of three (also exact but for pieces below the type's range), each piece multiplied with the same a^.  So
+// every product is exact and only the sums round.
+//
+// Both operands have the summed index t as their slow dimension: a stage holds 64 rows t of 128 columns of dy
+// and of a^ per CTA, in the 128-byte-swizzled layout with the output dimension contiguous, which the tensor cores
+// read without a transposition.  A pair of CTAs (cluster of two) owns a tile of 256 x 256 outputs: each CTA
+// brings 128 columns of dy and turns 128 columns of codes into bf16, so a code is converted once for 256 rows
+// of the tile.  The roles of a CTA's 20 warps:
+//   0      issues the copies of dy, codes and exponent bytes (TMA, three rings of stages)
+//   1      issues the products (in the pair's first CTA)
+//   3      passes on that dy has landed, and clears what a ragged stage holds of the next worker's rows
+//   4-11   add finished segments to fp32 sums in registers and write the tile
+//   12-19  convert codes, four warps a stage in turn
+// Tensor memory holds two accumulators.  The tensor cores cut off what does not fit when they add to one: the
+// relative error grows by 8e-9 a product step (4.1e-6 after 8192 rows, in one go), so a segment ends after
+// kSegmentSteps steps and its sum is added in fp32 outside, rounded to nearest (error then as a plain fp32 product's).
+// Tiles are dealt to the pairs; what is left after the last full round is cut along t into as many pieces as there
+// are pairs for it, whose sums go to scratch and are added in order by a second launch.
+#include <cuda.h>
+
 #include "qasg_lm.cuh"
 
 namespace qasg {
 
-constexpr int kWgTile = 64, kWgRows = 16;
+namespace {
 
-template <typename T>
-__global__ void __launch_bounds__(256)
-act_wgrad_kernel(WgradArgs a, ActView act, const __grid_constant__ RowShards shards) {
-  __shared__ float sd[kWgRows][kWgTile], sa[kWgRows][kWgTile];
-  const uint32_t m = blockIdx.z, n0 = blockIdx.y * kWgTile, k0 = blockIdx.x * kWgTile;
-  const uint32_t tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  chain_wait();
-  chain_trigger();
-  const T* dy = static_cast<const T*>(a.dy);
-  float acc[4][4] = {};
-  for (uint64_t t0 = shards.row0[m]; t0 < shards.row0[m + 1]; t0 += kWgRows) {
-    for (int i = threadIdx.x; i < kWgRows * kWgTile; i += 256) {
-      const uint64_t t = t0 + i / kWgTile;
-      const uint32_t c = i % kWgTile;
-      const bool in = t < shards.row0[m + 1];
-      sd[i / kWgTile][c] = in && n0 + c < a.out_cols ? to_float(dy[t * a.ld_dy + n0 + c]) : 0.f;
-      sa[i / kWgTile][c] = in && k0 + c < act.cols ? static_cast<float>(act.codes[t * act.ld_codes + k0 + c]) *
-                                                         act_unit(act.exps[t * act.ld_exps + (k0 + c) / kActBlock]) : 0.f;
+constexpr int kWgTile = 256;        // outputs of a pair's tile, each way
+constexpr int kWgHalf = 128;        // a CTA's share of either operand's columns
+constexpr int kWgRows = 64;         // rows t of a stage
+constexpr int kWgThreads = 640;
+constexpr int kFirstEpilogue = 4, kFirstConvert = 12, kGroupWarps = 4;  // two groups convert
+constexpr int kSegmentSteps = 64;   // product steps (of 16 rows and one piece of dy) an accumulator takes
+// Registers: the launch gives every thread kLaunchRegs; the roles then shift them (multiples of 8, a warpgroup at a
+// time), 4 warps at kIssueRegs + 8 at kSumRegs + 8 at kConvertRegs within the launch's 20 at kLaunchRegs.
+constexpr int kLaunchRegs = 96, kIssueRegs = 32, kSumRegs = 160, kConvertRegs = 64;
+static_assert(4 * kIssueRegs + 8 * kSumRegs + 8 * kConvertRegs <= 20 * kLaunchRegs, "registers of the launch");
+constexpr uint32_t kOperandBytes = kWgRows * kWgHalf * 2;  // 16 KB: two swizzle atoms of 64 columns
+constexpr uint32_t kCodeBytes = kWgRows * kWgHalf;
+constexpr uint32_t kCodeStage = kCodeBytes + kWgRows * 16;  // and 16 exponent bytes a row
+constexpr uint32_t kAtomBytes = kWgRows * 128;             // 64 columns x 64 rows
+constexpr int kTurnCols = 16, kTurnPitch = 17;
+constexpr long long kMaxWait = 1ll << 34;                  // bound of every wait in cycles (some seconds)
+
+// How dy reaches shared memory: bf16 rows on 16-byte boundaries by TMA, everything else through the converting
+// warps' registers, as 1, 2 or 3 bf16 pieces.
+template <typename T> constexpr int kPieces = 1;
+template <> constexpr int kPieces<__half> = 2;
+template <> constexpr int kPieces<float> = 3;
+// Stages of the rings: pieces of dy (A), converted codes (B), codes (C).
+template <int kP> constexpr int kStagesA = kP == 1 ? 5 : kP == 2 ? 3 : 2;
+template <int kP> constexpr int kStagesB = kP == 1 ? 4 : 3;
+constexpr int kStagesC = 6;
+template <int kP> constexpr uint32_t kWgSmem = kStagesA<kP> * kP * kOperandBytes + kStagesB<kP> * kOperandBytes + kStagesC * kCodeStage +
+                                               8 * 32 * kTurnPitch * 4 + 1024;
+
+struct WgradPlan {
+  RowShards shards;
+  uint32_t order[kMaxWorkers];  // workers, most rows first
+  uint32_t tiles_n, tiles_k;    // per worker
+  uint32_t whole;               // tiles summed by one pair each; the tiles after them are cut into pieces
+  uint32_t pieces, units;       // units = whole + pieces * (tiles - whole)
+};
+
+// ------------------------------------------------------------------ PTX
+__device__ __forceinline__ uint32_t smem_addr(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
+__device__ __forceinline__ uint32_t map_rank(uint32_t addr, uint32_t rank) {
+  uint32_t r;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ void barrier_init(uint32_t bar, uint32_t count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void barrier_expect(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void barrier_arrive_cluster(uint32_t cluster_bar) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+}
+__device__ __forceinline__ bool barrier_try(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n.reg .pred p;\n"
+      "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n"
+      "selp.u32 %0, 1, 0, p;\n}"
+      : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok != 0;
+}
+// Bounded wait: false once the wait ran out here or in another warp of the CTA.
+__device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity, volatile uint32_t* gave_up) {
+  if (barrier_try(bar, parity)) return true;
+  const long long began = clock64();
+  while (!barrier_try(bar, parity)) {
+    if (*gave_up) return false;
+    if (clock64() - began > kMaxWait) {
+      *gave_up = 1u;
+      return false;
     }
-    __syncthreads();
-#pragma unroll
-    for (int r = 0; r < kWgRows; ++r)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(sd[r][ty * 4 + i], sa[r][tx * 4 + j], acc[i][j]);
-    __syncthreads();
   }
-  for (int i = 0; i < 4; ++i)
-    for (int j = 0; j < 4; ++j) {
-      const uint32_t n = n0 + ty * 4 + i, k = k0 + tx * 4 + j;
-      if (n >= a.out_cols || k >= act.cols) continue;
-      float* g = a.g + m * a.ld_g + n * a.ld_w + k;
-      const float v = a.weight ? acc[i][j] * a.weight[k] : acc[i][j];
-      *g = a.accumulate ? *g + v : v;
-    }
+  return true;
+}
+// The same for what is in flight when a warp has given up: it ends by itself, soon.
+__device__ __forceinline__ void barrier_drain(uint32_t bar, uint32_t parity) {
+  const long long began = clock64();
+  while (!barrier_try(bar, parity) && clock64() - began < (1ll << 28)) {}
+}
+__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+               "l"(map), "r"(x), "r"(y), "r"(bar)
+               : "memory");
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.aligned;\nbarrier.cluster.wait.aligned;" ::: "memory");
 }
 
-uint64_t act_wgrad_scratch_bytes(uint64_t, uint64_t, uint32_t) { return 16; }
+// Operand with its output dimension contiguous: atoms of 64 columns x 8 rows (1 KB, 128-byte swizzle); the next
+// eight rows follow 1 KB on, the next 64 columns one atom column (kAtomBytes) on.
+__device__ __forceinline__ uint64_t operand_desc(uint32_t addr) {
+  return static_cast<uint64_t>((addr & 0x3ffffu) >> 4) | (static_cast<uint64_t>(kAtomBytes >> 4) << 16) |
+         (static_cast<uint64_t>(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
+}
+// fp32 accumulators, bf16 operands, both with the output dimension contiguous, 256 x 256.
+constexpr uint32_t kInstruction = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16) | ((kWgTile >> 3) << 17) |
+                                  ((kWgTile >> 4) << 24);
+__device__ __forceinline__ void mma_pair(uint32_t acc, uint64_t a, uint64_t b, bool add) {
+  asm volatile(
+      "{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\n"
+      "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(acc), "l"(a), "l"(b), "r"(kInstruction),
+      "r"(static_cast<uint32_t>(add))
+      : "memory");
+}
+// Arrives on the barrier at this offset in both CTAs once the products issued so far have completed.
+__device__ __forceinline__ void mma_commit(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
+               "h"(static_cast<uint16_t>(3))
+               : "memory");
+}
+__device__ __forceinline__ void tmem_load8(uint32_t addr, uint32_t (&r)[8]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(addr));
+}
+__device__ __forceinline__ void tmem_loaded() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+template <int kRegs> __device__ __forceinline__ void more_registers() {
+  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegs));
+}
+template <int kRegs> __device__ __forceinline__ void fewer_registers() {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegs));
+}
 
-int launch_act_wgrad(int dtype, const WgradArgs& a, const ActView& act, const RowShards& shards, const LaunchShape& shape,
-                     cudaStream_t stream) {
-  with_dtype(dtype, [&](auto t) {
-    using T = decltype(t);
-    launch_lm(act_wgrad_kernel<T>, dim3((act.cols + kWgTile - 1) / kWgTile, (a.out_cols + kWgTile - 1) / kWgTile, a.M), 256, 0,
-              1, stream, shape.chained, a, act, shards);
-  });
-  return 1;
+// A place in a ring of n stages.
+template <int n> struct Ring {
+  uint32_t at, phase;
+  __device__ __forceinline__ void next() {
+    if (++at == n) at = 0, phase ^= 1u;
+  }
+  __device__ __forceinline__ void back() {
+    if (at == 0) at = n, phase ^= 1u;
+    --at;
+  }
+};
+
+// ------------------------------------------------------------------ units of work
+struct TileWork {
+  uint64_t row0, row1;  // rows t
+  uint32_t worker, n0, k0;
+  int32_t slot;         // the piece's place in scratch, -1: the outputs are final
+};
+__device__ __forceinline__ TileWork unit_of(const WgradPlan& p, uint32_t u) {
+  uint32_t tile = u, piece = 0, pieces = 1;
+  if (u >= p.whole) {
+    pieces = p.pieces;
+    tile = p.whole + (u - p.whole) / pieces;
+    piece = (u - p.whole) % pieces;
+  }
+  const uint32_t per_worker = p.tiles_n * p.tiles_k, w = tile / per_worker, i = tile - w * per_worker;
+  // tiles in strips of eight rows of tiles, so that the pairs at work share operands in L2
+  const uint32_t strip = i / (8 * p.tiles_k), high = min(8u, p.tiles_n - 8 * strip), j = i - strip * 8 * p.tiles_k;
+  TileWork r;
+  r.worker = p.order[w];
+  r.n0 = (8 * strip + j % high) * kWgTile;
+  r.k0 = (j / high) * kWgTile;
+  const uint64_t first = p.shards.row0[r.worker], steps = (p.shards.row0[r.worker + 1] - first + kWgRows - 1) / kWgRows;
+  r.row0 = first + steps * piece / pieces * kWgRows;
+  r.row1 = min(first + steps * (piece + 1) / pieces * kWgRows, p.shards.row0[r.worker + 1]);
+  if (r.row0 > r.row1) r.row0 = r.row1;
+  r.slot = pieces > 1 ? static_cast<int32_t>(u - p.whole) : -1;
+  return r;
+}
+
+// Eight codes (two words) times their unit, as four words of bf16 pairs.  A byte c = 128 s + l (s its sign bit) is
+// taken apart into the bf16 numbers 128 + l and -128 - 128 s, whose sum is the code.
+__device__ __forceinline__ uint32_t code_pair(uint32_t two, uint32_t unit2) {
+  const uint32_t low = (two & 0x007f007fu) | 0x43004300u, sign = (two & 0x00800080u) | 0xc300c300u;
+  const __nv_bfloat162 v = __hmul2(__hadd2(*reinterpret_cast<const __nv_bfloat162*>(&low), *reinterpret_cast<const __nv_bfloat162*>(&sign)),
+                                   *reinterpret_cast<const __nv_bfloat162*>(&unit2));
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ uint4 code_octet(uint32_t w0, uint32_t w1, uint32_t unit2) {
+  uint4 r;
+  r.x = code_pair(__byte_perm(w0, 0u, 0x4140), unit2);
+  r.y = code_pair(__byte_perm(w0, 0u, 0x4342), unit2);
+  r.z = code_pair(__byte_perm(w1, 0u, 0x4140), unit2);
+  r.w = code_pair(__byte_perm(w1, 0u, 0x4342), unit2);
+  return r;
+}
+// Place of 16-byte chunk `chunk` (eight columns) of row t in an operand.
+__device__ __forceinline__ uint32_t chunk_offset(uint32_t t, uint32_t chunk) {
+  return (chunk >> 3) * kAtomBytes + t * 128 + (((chunk & 7u) ^ (t & 7u)) << 4);
+}
+__device__ __forceinline__ void store_shared(uint32_t addr, uint4 v) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+__device__ __forceinline__ uint4 load_shared(uint32_t addr) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint32_t load_shared_byte(uint32_t addr) {
+  uint32_t v;
+  asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+  return v;
+}
+
+// The raw words of columns [c, c + 8) of a row of n values, zeros past its end; any alignment.
+template <typename T> __device__ __forceinline__ Unit<T> load_raw(const T* row, uint32_t c, uint32_t n) {
+  if (c + kUnit <= n && is_aligned16(row + c)) return load_unit(row + c);
+  Unit<T> u;
+#pragma unroll
+  for (int i = 0; i < static_cast<int>(sizeof(u) / 4); ++i) {
+    constexpr int kEach = 4 / sizeof(T);
+    u.w[i] = 0u;
+#pragma unroll
+    for (int j = 0; j < kEach; ++j)
+      if (c + i * kEach + j < n) {
+        const T v = row[c + i * kEach + j];
+        if (sizeof(T) == 2) u.w[i] |= static_cast<uint32_t>(*reinterpret_cast<const uint16_t*>(&v)) << (16 * j);
+        else u.w[i] = *reinterpret_cast<const uint32_t*>(&v);
+      }
+  }
+  return u;
+}
+
+// ------------------------------------------------------------------ kernel
+template <typename T, bool kTma>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWgThreads, 1)
+act_wgrad_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_constant__ CUtensorMap map_codes,
+                 const __grid_constant__ CUtensorMap map_exps, const __grid_constant__ WgradPlan plan,
+                 const __grid_constant__ WgradArgs a, uint32_t cols, unsigned int* __restrict__ status) {
+  constexpr int kP = kPieces<T>, kA = kStagesA<kP>, kB = kStagesB<kP>;
+  constexpr uint32_t kStageA = kP * kOperandBytes;
+  constexpr int kSegment = kSegmentSteps / (kWgRows / 16) / kP;  // stages of a segment
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ __align__(8) uint64_t bars[3 * kA + 2 * kB + 2 * kStagesC + 4];
+  __shared__ uint32_t tmem_base, gave_up;
+  __shared__ Ring<kA> last_a;
+  __shared__ Ring<kB> last_b;
+  const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  uint32_t rank;
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+  const uint32_t pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+  const uint32_t at_a = (smem_addr(smem_raw) + 1023u) & ~1023u, at_b = at_a + kA * kStageA, at_c = at_b + kB * kOperandBytes,
+                 at_turn = at_c + kStagesC * kCodeStage;
+  // full: a copy has landed in this CTA; ready: both CTAs' part of a stage can be multiplied (the first CTA's
+  // barriers count); empty: a stage may be overwritten
+  const uint32_t full_a = smem_addr(bars), ready_a = full_a + 8 * kA, empty_a = ready_a + 8 * kA, ready_b = empty_a + 8 * kA,
+                 empty_b = ready_b + 8 * kB, full_c = empty_b + 8 * kB, empty_c = full_c + 8 * kStagesC,
+                 acc_full = empty_c + 8 * kStagesC, acc_empty = acc_full + 16;
+  if (tid == 0) {
+    gave_up = 0u;
+    for (int s = 0; s < kA; ++s) {
+      barrier_init(full_a + 8 * s, 1);
+      barrier_init(ready_a + 8 * s, kTma ? 2 : 2 * kGroupWarps);
+      barrier_init(empty_a + 8 * s, 1);
+    }
+    for (int s = 0; s < kB; ++s) {
+      barrier_init(ready_b + 8 * s, 2 * kGroupWarps);
+      barrier_init(empty_b + 8 * s, 1);
+    }
+    for (int s = 0; s < kStagesC; ++s) {
+      barrier_init(full_c + 8 * s, 1);
+      barrier_init(empty_c + 8 * s, kGroupWarps);
+    }
+    for (int i = 0; i < 2; ++i) {
+      barrier_init(acc_full + 8 * i, 1);
+      barrier_init(acc_empty + 8 * i, 16);
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 2) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&tmem_base)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  cluster_sync();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  const uint32_t tmem = tmem_base;
+  chain_wait();
+  chain_trigger();
+
+  if (warp < kFirstEpilogue) {
+    fewer_registers<kIssueRegs>();
+    if (warp == 0 && lane == 0) {
+      // copies
+      Ring<kA> ra = {0, 0};
+      Ring<kStagesC> rc = {0, 0};
+      uint32_t issued = 0;
+      bool ok = true;
+      for (uint32_t u = pair; u < plan.units && ok; u += pairs) {
+        const TileWork w = unit_of(plan, u);
+        const int n = static_cast<int>(w.n0 + rank * kWgHalf), k = static_cast<int>(w.k0 + rank * kWgHalf);
+        for (uint32_t y = static_cast<uint32_t>(w.row0); y < static_cast<uint32_t>(w.row1); y += kWgRows) {
+          if (!(ok = barrier_wait(empty_c + 8 * rc.at, rc.phase ^ 1u, &gave_up))) break;
+          const uint32_t bar_c = full_c + 8 * rc.at, c = at_c + rc.at * kCodeStage;
+          barrier_expect(bar_c, kCodeStage);
+          tma_load(c, &map_codes, k, y, bar_c);
+          tma_load(c + kCodeBytes, &map_exps, (k / kActBlock) & ~15, y, bar_c);
+          rc.next();
+          if (kTma) {
+            if (!(ok = barrier_wait(empty_a + 8 * ra.at, ra.phase ^ 1u, &gave_up))) break;
+            const uint32_t bar_a = full_a + 8 * ra.at, at = at_a + ra.at * kStageA;
+            barrier_expect(bar_a, kOperandBytes);
+            tma_load(at, &map_dy, n, y, bar_a);
+            tma_load(at + kAtomBytes, &map_dy, n + 64, y, bar_a);
+            ra.next();
+          }
+          ++issued;
+        }
+      }
+      if (!ok) {  // gave up: the copies in flight land before the CTA leaves
+        for (uint32_t i = min(issued + 1, static_cast<uint32_t>(kStagesC)); i > 0; --i) {
+          rc.back();
+          barrier_drain(full_c + 8 * rc.at, rc.phase);
+        }
+        for (uint32_t i = kTma ? min(issued, static_cast<uint32_t>(kA)) : 0; i > 0; --i) {
+          ra.back();
+          barrier_drain(full_a + 8 * ra.at, ra.phase);
+        }
+      }
+    } else if (warp == 1 && lane == 0) {
+      Ring<kA> ra = {0, 0};
+      Ring<kB> rb = {0, 0};
+      Ring<2> acc = {0, 0};
+      bool ok = true;
+      for (uint32_t u = pair; u < plan.units && ok; u += pairs) {
+        const TileWork w = unit_of(plan, u);
+        uint32_t left = static_cast<uint32_t>((w.row1 - w.row0 + kWgRows - 1) / kWgRows);
+        while (left && ok) {
+          const uint32_t stages = min(left, static_cast<uint32_t>(kSegment));
+          left -= stages;
+          if (rank == 0) {  // products
+            if (!(ok = barrier_wait(acc_empty + 8 * acc.at, acc.phase ^ 1u, &gave_up))) break;
+            bool add = false;
+            for (uint32_t i = 0; i < stages; ++i) {
+              if (!(ok = barrier_wait(ready_b + 8 * rb.at, rb.phase, &gave_up))) break;
+              if (!(ok = barrier_wait(ready_a + 8 * ra.at, ra.phase, &gave_up))) break;
+              asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+              const uint32_t pa = at_a + ra.at * kStageA, pb = at_b + rb.at * kOperandBytes;
+#pragma unroll
+              for (int j = 0; j < kWgRows / 16; ++j) {
+                const uint64_t b = operand_desc(pb + j * 2048);
+#pragma unroll
+                for (int p = 0; p < kP; ++p) {
+                  mma_pair(tmem + acc.at * kWgTile, operand_desc(pa + p * kOperandBytes + j * 2048), b, add);
+                  add = true;
+                }
+              }
+              mma_commit(empty_a + 8 * ra.at);
+              mma_commit(empty_b + 8 * rb.at);
+              ra.next(), rb.next();
+            }
+            mma_commit(acc_full + 8 * acc.at);
+            if (!ok) barrier_drain(acc_full + 8 * acc.at, acc.phase);  // gave up: the products in flight end first
+            acc.next();
+          } else {
+            for (uint32_t i = 0; i < stages; ++i) ra.next(), rb.next();
+          }
+        }
+      }
+      last_a = ra, last_b = rb;
+    } else if (warp == 3 && kTma) {
+      Ring<kA> ra = {0, 0};
+      const uint32_t ready_of_first = map_rank(ready_a, 0);
+      bool ok = true;
+      for (uint32_t u = pair; u < plan.units && ok; u += pairs) {
+        const TileWork w = unit_of(plan, u);
+        uint32_t rows = static_cast<uint32_t>(w.row1 - w.row0);
+        while (rows) {
+          if (!(ok = __all_sync(0xffffffffu, barrier_wait(full_a + 8 * ra.at, ra.phase, &gave_up)))) break;
+          if (rows < kWgRows) {  // rows of another worker came with the copy: they must not meet 0 * inf
+            for (uint32_t i = lane; i < (kWgRows - rows) * 16; i += 32)
+              store_shared(at_a + ra.at * kStageA + chunk_offset(rows + (i >> 4), i & 15u), make_uint4(0u, 0u, 0u, 0u));
+          }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) barrier_arrive_cluster(ready_of_first + 8 * ra.at);
+          ra.next();
+          rows -= min(rows, static_cast<uint32_t>(kWgRows));
+        }
+      }
+    }
+  } else if (warp >= kFirstConvert) {
+    // conversion: the groups of warps take stages in turn; a thread takes 16 columns (seg) of rows r, r + 16, ...
+    fewer_registers<kConvertRegs>();
+    constexpr int kLoads = sizeof(T) == 4 ? 2 : 4;  // chunks of dy a thread has in flight
+    const uint32_t group = (warp - kFirstConvert) / kGroupWarps, ctid = tid - (kFirstConvert + group * kGroupWarps) * 32;
+    const uint32_t seg = ctid & 7u, chunk = ctid & 15u;
+    const T* dy = static_cast<const T*>(a.dy);
+    const uint32_t ready_a_first = map_rank(ready_a, 0), ready_b_first = map_rank(ready_b, 0);
+    Ring<kA> ra = {0, 0};
+    Ring<kB> rb = {0, 0};
+    Ring<kStagesC> rc = {0, 0};
+    uint32_t turn = 0;
+    bool ok = true;
+    for (uint32_t u = pair; u < plan.units && ok; u += pairs) {
+      const TileWork w = unit_of(plan, u);
+      const uint32_t exp_at = (((w.k0 + rank * kWgHalf) / kActBlock) & 15u) + (seg >> 1);
+      const uint32_t n = w.n0 + rank * kWgHalf + chunk * kUnit;
+      for (uint64_t t = w.row0; t < w.row1; t += kWgRows, ra.next(), rb.next(), rc.next(), turn ^= 1u) {
+        if (turn != group) continue;
+        const uint32_t rows = static_cast<uint32_t>(min(static_cast<uint64_t>(kWgRows), w.row1 - t));
+        Unit<T> raw[kTma ? 1 : kLoads];
+        auto load = [&](int batch) {
+#pragma unroll
+          for (int i = 0; i < kLoads; ++i) {
+            const uint32_t r = (ctid >> 4) + 8 * (batch * kLoads + i);
+            raw[kTma ? 0 : i] = load_raw<T>(dy + (t + r) * a.ld_dy, n, r < rows ? a.out_cols : 0u);
+          }
+        };
+        if (!kTma) load(0);
+        if (!(ok = __all_sync(0xffffffffu, barrier_wait(full_c + 8 * rc.at, rc.phase, &gave_up)))) break;
+        if (!(ok = __all_sync(0xffffffffu, barrier_wait(empty_b + 8 * rb.at, rb.phase ^ 1u, &gave_up)))) break;
+        const uint32_t codes = at_c + rc.at * kCodeStage, out = at_b + rb.at * kOperandBytes;
+        uint4 c[4];
+        uint32_t b[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t r = (ctid >> 3) + 16 * i;
+          c[i] = load_shared(codes + r * kWgHalf + seg * 16);
+          b[i] = load_shared_byte(codes + kCodeBytes + r * 16 + exp_at);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t r = (ctid >> 3) + 16 * i;
+          const uint32_t unit = b[i] == kActNan ? 0x7fffu : (b[i] - 6u) << 7, unit2 = unit | (unit << 16);
+          uint4 lo = code_octet(c[i].x, c[i].y, unit2), hi = code_octet(c[i].z, c[i].w, unit2);
+          if (r >= rows) lo = hi = make_uint4(0u, 0u, 0u, 0u);
+          // segments of the second atom store their odd chunk first: eight threads then cover all banks
+          const bool odd_first = seg >= 4;
+          store_shared(out + chunk_offset(r, 2 * seg + (odd_first ? 1 : 0)), odd_first ? hi : lo);
+          store_shared(out + chunk_offset(r, 2 * seg + (odd_first ? 0 : 1)), odd_first ? lo : hi);
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) {
+          barrier_arrive_cluster(empty_c + 8 * rc.at);
+          barrier_arrive_cluster(ready_b_first + 8 * rb.at);
+        }
+        if (!kTma) {
+          if (!(ok = __all_sync(0xffffffffu, barrier_wait(empty_a + 8 * ra.at, ra.phase ^ 1u, &gave_up)))) break;
+          for (int batch = 0; batch < 8 / kLoads; ++batch) {
+            if (batch) load(batch);
+#pragma unroll
+            for (int i = 0; i < (kTma ? 1 : kLoads); ++i) {
+              float v[kUnit];
+              unit_floats(raw[i], v);
+#pragma unroll
+              for (int p = 0; p < kP; ++p) {  // the leading eight bits as bf16, then those of what is left
+                uint32_t q[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                  q[j] = __byte_perm(__float_as_uint(v[2 * j]), __float_as_uint(v[2 * j + 1]), 0x7632);
+#pragma unroll
+                for (int j = 0; j < kUnit; ++j) {
+                  const float rest = v[j] - __uint_as_float(__float_as_uint(v[j]) & 0xffff0000u);
+                  v[j] = fabsf(v[j]) < INFINITY ? rest : 0.f;
+                }
+                store_shared(at_a + ra.at * kStageA + p * kOperandBytes + chunk_offset((ctid >> 4) + 8 * (batch * kLoads + i), chunk),
+                             make_uint4(q[0], q[1], q[2], q[3]));
+              }
+            }
+          }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) barrier_arrive_cluster(ready_a_first + 8 * ra.at);
+        }
+      }
+    }
+  } else {
+    // sums and output: a warp takes 32 rows (quarter) and 128 columns (half) of the CTA's 128 x 256.  On the way
+    // out 16 columns at a time are turned in shared memory, so that a store covers 64 bytes of two rows.
+    more_registers<kSumRegs>();
+    const uint32_t quarter = warp & 3u, half = (warp - kFirstEpilogue) >> 2;
+    float* turn = reinterpret_cast<float*>(smem_raw + (at_turn - smem_addr(smem_raw))) + (warp - kFirstEpilogue) * 32 * kTurnPitch;
+    const uint32_t acc_empty_first = map_rank(acc_empty, 0);
+    Ring<2> acc = {0, 0};
+    bool ok = true;
+    for (uint32_t u = pair; u < plan.units && ok; u += pairs) {
+      const TileWork w = unit_of(plan, u);
+      float sum[kWgHalf];
+#pragma unroll
+      for (int i = 0; i < kWgHalf; ++i) sum[i] = 0.f;
+      for (uint32_t left = static_cast<uint32_t>((w.row1 - w.row0 + kWgRows - 1) / kWgRows); left;
+           left -= min(left, static_cast<uint32_t>(kSegment))) {
+        if (!(ok = __all_sync(0xffffffffu, barrier_wait(acc_full + 8 * acc.at, acc.phase, &gave_up)))) break;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        const uint32_t from = tmem + acc.at * kWgTile + half * kWgHalf + (quarter << 21);
+#pragma unroll
+        for (int i = 0; i < kWgHalf; i += 8) {
+          uint32_t r[8];
+          tmem_load8(from + i, r);
+          tmem_loaded();
+#pragma unroll
+          for (int j = 0; j < 8; ++j) sum[i + j] += __uint_as_float(r[j]);
+        }
+        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) barrier_arrive_cluster(acc_empty_first + 8 * acc.at);
+        acc.next();
+      }
+      if (!ok) break;
+      const uint32_t row = rank * kWgHalf + quarter * 32 + (lane >> 4), col = half * kWgHalf + (lane & 15u);
+#pragma unroll
+      for (int c = 0; c < kWgHalf; c += kTurnCols) {
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < kTurnCols; ++i) turn[lane * kTurnPitch + i] = sum[c + i];
+        __syncwarp();
+        const float* from = turn + (lane >> 4) * kTurnPitch + (lane & 15u);
+        const uint32_t k = w.k0 + col + c, n = w.n0 + row;
+        if (w.slot >= 0) {
+          float* out = static_cast<float*>(a.scratch) + (static_cast<uint64_t>(w.slot) * kWgTile + row) * kWgTile + col + c;
+#pragma unroll 8
+          for (int i = 0; i < 16; ++i) out[2 * i * kWgTile] = from[2 * i * kTurnPitch];
+        } else if (k < cols && n < a.out_cols) {
+          const float scale = a.weight ? __ldg(a.weight + k) : 1.f;
+          float* out = a.g + w.worker * a.ld_g + n * a.ld_w + k;
+          const int rows = static_cast<int>(min(16u, (a.out_cols - n + 1) / 2));
+          if (a.accumulate) {
+#pragma unroll 4
+            for (int i = 0; i < rows; ++i) out[2 * i * a.ld_w] += from[2 * i * kTurnPitch] * scale;
+          } else {
+#pragma unroll 4
+            for (int i = 0; i < rows; ++i) out[2 * i * a.ld_w] = from[2 * i * kTurnPitch] * scale;
+          }
+        }
+      }
+    }
+  }
+  __syncwarp();
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  if (tid == 32) {  // the arrivals that release the last stages land before the CTA leaves
+    bool ok = !gave_up;
+    for (int i = 0; i < kA && ok; ++i, last_a.next()) ok = barrier_wait(empty_a + 8 * last_a.at, last_a.phase ^ 1u, &gave_up);
+    for (int i = 0; i < kB && ok; ++i, last_b.next()) ok = barrier_wait(empty_b + 8 * last_b.at, last_b.phase ^ 1u, &gave_up);
+  }
+  __syncwarp();
+  cluster_sync();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  if (tid == 0 && gave_up) atomicOr(status, kFlagTimeout);
+  if (warp == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+}
+
+// Adds the pieces of the tiles after plan.whole, in order.  A CTA takes eight rows of a tile.
+__global__ void __launch_bounds__(256)
+piece_sum_kernel(const __grid_constant__ WgradPlan plan, WgradArgs a, uint32_t cols) {
+  const uint32_t i = blockIdx.x / 32, r = (blockIdx.x % 32) * 8;
+  chain_wait();
+  chain_trigger();
+  const TileWork w = unit_of(plan, plan.whole + i * plan.pieces);
+  const uint32_t k = w.k0 + threadIdx.x;
+  if (k >= cols) return;
+  const float scale = a.weight ? __ldg(a.weight + k) : 1.f;
+  const float* part = static_cast<const float*>(a.scratch) + (static_cast<uint64_t>(i) * plan.pieces * kWgTile + r) * kWgTile + threadIdx.x;
+  float s[8] = {};
+  for (uint32_t p = 0; p < plan.pieces; ++p, part += kWgTile * kWgTile)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s[j] += __ldcg(part + j * kWgTile);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const uint32_t n = w.n0 + r + j;
+    if (n >= a.out_cols) break;
+    float* out = a.g + w.worker * a.ld_g + n * a.ld_w + k;
+    *out = a.accumulate ? *out + s[j] * scale : s[j] * scale;
+  }
+}
+
+typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiled encode_tiled() {
+  static const EncodeTiled fn = [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &found) != cudaSuccess) p = nullptr;
+    return reinterpret_cast<EncodeTiled>(p);
+  }();
+  return fn;
+}
+
+// Rows of `cols` elements in boxes of box x kWgRows; outside the matrix reads as zeros.
+bool make_map(CUtensorMap* map, CUtensorMapDataType type, uint32_t size, const void* base, uint64_t cols, uint64_t rows, uint64_t ld,
+              uint32_t box, bool swizzle) {
+  const cuuint64_t dims[2] = {cols, rows}, strides[1] = {ld * size};
+  const cuuint32_t boxes[2] = {box, kWgRows}, steps[2] = {1, 1};
+  return encode_tiled()(map, type, 2, const_cast<void*>(base), dims, strides, boxes, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                        swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+constexpr uint32_t kMaxPairs = 80;      // pieces of cut tiles at a time
+constexpr uint32_t kMinPieceSteps = 4;  // stages of a piece: shorter ones cost more in sums than they save
+
+}  // namespace
+
+uint64_t act_wgrad_scratch_bytes(uint64_t out_cols, uint64_t cols, uint32_t M) {
+  (void)out_cols, (void)cols, (void)M;
+  return static_cast<uint64_t>(kMaxPairs) * kWgTile * kWgTile * sizeof(float);
+}
+
+int launch_act_wgrad(int dtype, const WgradArgs& a, const ActView& act, const RowShards& shards, unsigned int* status,
+                     const LaunchShape& shape, cudaStream_t stream) {
+  if (!encode_tiled()) return -1;
+  WgradPlan plan;
+  plan.shards = shards;
+  plan.tiles_n = (a.out_cols + kWgTile - 1) / kWgTile;
+  plan.tiles_k = (act.cols + kWgTile - 1) / kWgTile;
+  for (uint32_t m = 0; m < a.M; ++m) {  // most rows first: the short ones fill up the last round
+    const uint64_t rows = shards.row0[m + 1] - shards.row0[m];
+    uint32_t i = m;
+    for (; i > 0 && shards.row0[plan.order[i - 1] + 1] - shards.row0[plan.order[i - 1]] < rows; --i) plan.order[i] = plan.order[i - 1];
+    plan.order[i] = m;
+  }
+  const uint32_t pairs = min(kMaxPairs, static_cast<uint32_t>(shape.sm_count / 2));
+  const uint32_t tiles = plan.tiles_n * plan.tiles_k * a.M, left = tiles % pairs;
+  const uint32_t steps = static_cast<uint32_t>((shards.row0[plan.order[0] + 1] - shards.row0[plan.order[0]] + kWgRows - 1) / kWgRows);
+  plan.pieces = left ? min(pairs / left, steps / kMinPieceSteps) : 1u;
+  if (plan.pieces < 2) plan.pieces = 1;
+  plan.whole = plan.pieces > 1 ? tiles - left : tiles;
+  plan.units = plan.whole + plan.pieces * (tiles - plan.whole);
+
+  const bool tma = dtype == kDtypeBf16 && a.ld_dy % 8 == 0 && (reinterpret_cast<uintptr_t>(a.dy) & 15u) == 0;
+  CUtensorMap map_dy = {}, map_codes = {}, map_exps = {};
+  bool ok = true;
+  if (act.rows) {  // without rows no copy is issued
+    const uint32_t padded = (act.cols + kActBlock - 1) / kActBlock * kActBlock;
+    if (tma) ok &= make_map(&map_dy, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, a.dy, a.out_cols, act.rows, a.ld_dy, 64, true);
+    ok &= make_map(&map_codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, act.codes, padded, act.rows, act.ld_codes, kWgHalf, false);
+    ok &= make_map(&map_exps, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, act.exps, act.ld_exps, act.rows, act.ld_exps, 16, false);
+  }
+  if (!ok) return -1;
+  const dim3 grid(2 * min(pairs, plan.units));
+  auto go = [&](auto kernel, uint32_t smem) {
+    cudaFuncAttributes attributes;
+    ok &= cudaFuncGetAttributes(&attributes, kernel) == cudaSuccess && attributes.numRegs == kLaunchRegs;
+    ok &= cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) == cudaSuccess;
+    if (ok) launch_lm(kernel, grid, kWgThreads, smem, 1, stream, shape.chained, map_dy, map_codes, map_exps, plan, a, act.cols, status);
+  };
+  if (tma) go(act_wgrad_kernel<__nv_bfloat16, true>, kWgSmem<1>);
+  else if (dtype == kDtypeBf16) go(act_wgrad_kernel<__nv_bfloat16, false>, kWgSmem<1>);
+  else if (dtype == kDtypeF16) go(act_wgrad_kernel<__half, false>, kWgSmem<2>);
+  else go(act_wgrad_kernel<float, false>, kWgSmem<3>);
+  if (!ok) return -1;
+  if (plan.pieces == 1) return 1;
+  launch_lm(piece_sum_kernel, dim3((tiles - plan.whole) * 32), 256, 0, 1, stream, shape.chained, plan, a, act.cols);
+  return 2;
 }
 
 }  // namespace qasg
