@@ -11,7 +11,7 @@
 // read without a transposition.  A pair of CTAs (cluster of two) owns a tile of 256 x 256 outputs: each CTA
 // brings 128 columns of dy and turns 128 columns of codes into bf16, so a code is converted once for 256 rows
 // of the tile.  The roles of a CTA's 20 warps:
-//   0      issues the copies of dy, codes and exponent bytes (TMA, three rings of stages)
+//   0      issues the copies of dy, codes and exponent bytes (TMA, two rings of stages)
 //   1      issues the products (in the pair's first CTA)
 //   3      passes on that dy has landed, and clears what a ragged stage holds of the next worker's rows
 //   4-11   add finished segments to fp32 sums in registers and write the tile
@@ -37,7 +37,7 @@ constexpr int kFirstEpilogue = 4, kFirstConvert = 12, kGroupWarps = 4;  // two g
 constexpr int kSegmentSteps = 64;   // product steps (of 16 rows and one piece of dy) an accumulator takes
 // Registers: the launch gives every thread kLaunchRegs; the roles then shift them (multiples of 8, a warpgroup at a
 // time), 4 warps at kIssueRegs + 8 at kSumRegs + 8 at kConvertRegs within the launch's 20 at kLaunchRegs.
-constexpr int kLaunchRegs = 96, kIssueRegs = 32, kSumRegs = 160, kConvertRegs = 64;
+constexpr int kLaunchRegs = 96, kIssueRegs = 48, kSumRegs = 152, kConvertRegs = 64;
 static_assert(4 * kIssueRegs + 8 * kSumRegs + 8 * kConvertRegs <= 20 * kLaunchRegs, "registers of the launch");
 constexpr uint32_t kOperandBytes = kWgRows * kWgHalf * 2;  // 16 KB: two swizzle atoms of 64 columns
 constexpr uint32_t kCodeBytes = kWgRows * kWgHalf;
@@ -51,12 +51,11 @@ constexpr long long kMaxWait = 1ll << 34;                  // bound of every wai
 template <typename T> constexpr int kPieces = 1;
 template <> constexpr int kPieces<__half> = 2;
 template <> constexpr int kPieces<float> = 3;
-// Stages of the rings: pieces of dy (A), converted codes (B), codes (C).
-template <int kP> constexpr int kStagesA = kP == 1 ? 5 : kP == 2 ? 3 : 2;
-template <int kP> constexpr int kStagesB = kP == 1 ? 4 : 3;
-constexpr int kStagesC = 6;
-template <int kP> constexpr uint32_t kWgSmem = kStagesA<kP> * kP * kOperandBytes + kStagesB<kP> * kOperandBytes + kStagesC * kCodeStage +
-                                               8 * 32 * kTurnPitch * 4 + 1024;
+// Stages of the two rings: operands (the pieces of dy, then the converted codes), and codes as they come.
+template <int kP> constexpr int kStages = kP == 1 ? 5 : kP == 2 ? 3 : 2;
+constexpr int kCodeStages = 4;
+template <int kP> constexpr uint32_t kStageBytes = (kP + 1) * kOperandBytes;
+template <int kP> constexpr uint32_t kWgSmem = kStages<kP> * kStageBytes<kP> + kCodeStages * kCodeStage + 8 * 32 * kTurnPitch * 4 + 1024;
 
 struct WgradPlan {
   RowShards shards;
@@ -80,13 +79,13 @@ __device__ __forceinline__ void barrier_expect(uint32_t bar, uint32_t bytes) {
   asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ void barrier_arrive_cluster(uint32_t cluster_bar) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
 __device__ __forceinline__ bool barrier_try(uint32_t bar, uint32_t parity) {
   uint32_t ok;
   asm volatile(
       "{\n.reg .pred p;\n"
-      "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n"
       "selp.u32 %0, 1, 0, p;\n}"
       : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
   return ok != 0;
@@ -104,6 +103,10 @@ __device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity, vola
   }
   return true;
 }
+// The same by all lanes of a warp, with one answer.
+__device__ __forceinline__ bool all_wait(uint32_t bar, uint32_t parity, volatile uint32_t* gave_up) {
+  return __all_sync(0xffffffffu, barrier_wait(bar, parity, gave_up));
+}
 // The same for what is in flight when a warp has given up: it ends by itself, soon.
 __device__ __forceinline__ void barrier_drain(uint32_t bar, uint32_t parity) {
   const long long began = clock64();
@@ -119,20 +122,24 @@ __device__ __forceinline__ void cluster_sync() {
 }
 
 // Operand with its output dimension contiguous: atoms of 64 columns x 8 rows (1 KB, 128-byte swizzle); the next
-// eight rows follow 1 KB on, the next 64 columns one atom column (kAtomBytes) on.
-__device__ __forceinline__ uint64_t operand_desc(uint32_t addr) {
-  return static_cast<uint64_t>((addr & 0x3ffffu) >> 4) | (static_cast<uint64_t>(kAtomBytes >> 4) << 16) |
-         (static_cast<uint64_t>(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
-}
+// eight rows follow 1 KB on, the next 64 columns one atom column (kAtomBytes) on.  The low word holds the address.
+constexpr uint32_t kDescHigh = (1024u >> 4) | (1u << 14) | (2u << 29);
+__device__ __forceinline__ uint32_t desc_low(uint32_t addr) { return ((addr & 0x3ffffu) >> 4) | ((kAtomBytes >> 4) << 16); }
 // fp32 accumulators, bf16 operands, both with the output dimension contiguous, 256 x 256.
 constexpr uint32_t kInstruction = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16) | ((kWgTile >> 3) << 17) |
                                   ((kWgTile >> 4) << 24);
-__device__ __forceinline__ void mma_pair(uint32_t acc, uint64_t a, uint64_t b, bool add) {
+__device__ __forceinline__ void mma_pair(uint32_t acc, uint32_t a_low, uint32_t b_low, uint32_t add) {
   asm volatile(
-      "{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\n"
-      "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(acc), "l"(a), "l"(b), "r"(kInstruction),
-      "r"(static_cast<uint32_t>(add))
+      "{\n.reg .pred p;\n.reg .b64 a, b;\n"
+      "mov.b64 a, {%1, %3};\nmov.b64 b, {%2, %3};\nsetp.ne.u32 p, %5, 0;\n"
+      "tcgen05.mma.cta_group::2.kind::f16 [%0], a, b, %4, p;\n}" ::"r"(acc), "r"(a_low), "r"(b_low), "r"(kDescHigh),
+      "r"(kInstruction), "r"(add)
       : "memory");
+}
+__device__ __forceinline__ bool elect_one() {
+  uint32_t r;
+  asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(r));
+  return r != 0;
 }
 // Arrives on the barrier at this offset in both CTAs once the products issued so far have completed.
 __device__ __forceinline__ void mma_commit(uint32_t bar) {
@@ -193,22 +200,28 @@ __device__ __forceinline__ TileWork unit_of(const WgradPlan& p, uint32_t u) {
   return r;
 }
 
-// Eight codes (two words) times their unit, as four words of bf16 pairs.  A byte c = 128 s + l (s its sign bit) is
-// taken apart into the bf16 numbers 128 + l and -128 - 128 s, whose sum is the code.
-__device__ __forceinline__ uint32_t code_pair(uint32_t two, uint32_t unit2) {
-  const uint32_t low = (two & 0x007f007fu) | 0x43004300u, sign = (two & 0x00800080u) | 0xc300c300u;
-  const __nv_bfloat162 v = __hmul2(__hadd2(*reinterpret_cast<const __nv_bfloat162*>(&low), *reinterpret_cast<const __nv_bfloat162*>(&sign)),
-                                   *reinterpret_cast<const __nv_bfloat162*>(&unit2));
-  return *reinterpret_cast<const uint32_t*>(&v);
+// Eight codes times their unit as four words of bf16 pairs, in the order 0 2 1 3 within each four (the tile's columns
+// are put back in order on the way out).  The bits of u = code + 128 are those of the bf16 number u * 2^-133, so
+// one multiply-add gives (u - 128) / 64 and one product with 2^E the value, all exact.  A NaN block has code 0 and
+// 2^E = inf: 0 * inf is the NaN that it stands for.
+__device__ __forceinline__ uint32_t code_pair(uint32_t two, uint32_t two_e) {
+  const uint32_t big = 0x7f007f00u, minus2 = 0xc000c000u;  // 2^127 and -2 as bf16 pairs
+  uint32_t v;
+  asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(v) : "r"(two), "r"(big), "r"(minus2));
+  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(v) : "r"(v), "r"(two_e));
+  return v;
 }
-__device__ __forceinline__ uint4 code_octet(uint32_t w0, uint32_t w1, uint32_t unit2) {
+__device__ __forceinline__ uint4 code_octet(uint2 w, uint32_t two_e) {
+  const uint32_t x = w.x ^ 0x80808080u, y = w.y ^ 0x80808080u;
   uint4 r;
-  r.x = code_pair(__byte_perm(w0, 0u, 0x4140), unit2);
-  r.y = code_pair(__byte_perm(w0, 0u, 0x4342), unit2);
-  r.z = code_pair(__byte_perm(w1, 0u, 0x4140), unit2);
-  r.w = code_pair(__byte_perm(w1, 0u, 0x4342), unit2);
+  r.x = code_pair(x & 0x00ff00ffu, two_e);
+  r.y = code_pair((x >> 8) & 0x00ff00ffu, two_e);
+  r.z = code_pair(y & 0x00ff00ffu, two_e);
+  r.w = code_pair((y >> 8) & 0x00ff00ffu, two_e);
   return r;
 }
+// Column of a group of 16 that column i of the product holds.
+__device__ __forceinline__ constexpr int product_column(int i) { return (i & ~3) | ((i & 1) << 1) | ((i >> 1) & 1); }
 // Place of 16-byte chunk `chunk` (eight columns) of row t in an operand.
 __device__ __forceinline__ uint32_t chunk_offset(uint32_t t, uint32_t chunk) {
   return (chunk >> 3) * kAtomBytes + t * 128 + (((chunk & 7u) ^ (t & 7u)) << 4);
@@ -216,14 +229,14 @@ __device__ __forceinline__ uint32_t chunk_offset(uint32_t t, uint32_t chunk) {
 __device__ __forceinline__ void store_shared(uint32_t addr, uint4 v) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
-__device__ __forceinline__ uint4 load_shared(uint32_t addr) {
-  uint4 v;
-  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+__device__ __forceinline__ uint2 load_shared2(uint32_t addr) {
+  uint2 v;
+  asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr) : "memory");
   return v;
 }
-__device__ __forceinline__ uint32_t load_shared_byte(uint32_t addr) {
+__device__ __forceinline__ uint32_t load_shared1(uint32_t addr) {
   uint32_t v;
-  asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+  asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
   return v;
 }
 
@@ -252,39 +265,32 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWgThreads, 1)
 act_wgrad_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_constant__ CUtensorMap map_codes,
                  const __grid_constant__ CUtensorMap map_exps, const __grid_constant__ WgradPlan plan,
                  const __grid_constant__ WgradArgs a, uint32_t cols, unsigned int* __restrict__ status) {
-  constexpr int kP = kPieces<T>, kA = kStagesA<kP>, kB = kStagesB<kP>;
-  constexpr uint32_t kStageA = kP * kOperandBytes;
+  constexpr int kP = kPieces<T>, kN = kStages<kP>;
+  constexpr uint32_t kStage = kStageBytes<kP>;
   constexpr int kSegment = kSegmentSteps / (kWgRows / 16) / kP;  // stages of a segment
   extern __shared__ uint8_t smem_raw[];
-  __shared__ __align__(8) uint64_t bars[3 * kA + 2 * kB + 2 * kStagesC + 4];
-  __shared__ uint32_t tmem_base, gave_up;
-  __shared__ Ring<kA> last_a;
-  __shared__ Ring<kB> last_b;
-  const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  __shared__ __align__(8) uint64_t bars[3 * kN + 2 * kCodeStages + 4];
+  __shared__ uint32_t tmem_base, gave_up, last_at, last_phase;
+  const uint32_t tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   uint32_t rank;
   asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
   const uint32_t pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
-  const uint32_t at_a = (smem_addr(smem_raw) + 1023u) & ~1023u, at_b = at_a + kA * kStageA, at_c = at_b + kB * kOperandBytes,
-                 at_turn = at_c + kStagesC * kCodeStage;
-  // full: a copy has landed in this CTA; ready: both CTAs' part of a stage can be multiplied (the first CTA's
-  // barriers count); empty: a stage may be overwritten
-  const uint32_t full_a = smem_addr(bars), ready_a = full_a + 8 * kA, empty_a = ready_a + 8 * kA, ready_b = empty_a + 8 * kA,
-                 empty_b = ready_b + 8 * kB, full_c = empty_b + 8 * kB, empty_c = full_c + 8 * kStagesC,
-                 acc_full = empty_c + 8 * kStagesC, acc_empty = acc_full + 16;
+  const uint32_t at_ring = (smem_addr(smem_raw) + 1023u) & ~1023u, at_codes = at_ring + kN * kStage,
+                 at_turn = at_codes + kCodeStages * kCodeStage;
+  // full: a copy has landed in this CTA (of dy, of codes); ready: both CTAs' part of a stage can be multiplied (the
+  // first CTA's barriers count); empty: a stage may be overwritten
+  const uint32_t full = smem_addr(bars), ready = full + 8 * kN, empty = ready + 8 * kN, code_full = empty + 8 * kN,
+                 code_empty = code_full + 8 * kCodeStages, acc_full = code_empty + 8 * kCodeStages, acc_empty = acc_full + 16;
   if (tid == 0) {
     gave_up = 0u;
-    for (int s = 0; s < kA; ++s) {
-      barrier_init(full_a + 8 * s, 1);
-      barrier_init(ready_a + 8 * s, kTma ? 2 : 2 * kGroupWarps);
-      barrier_init(empty_a + 8 * s, 1);
+    for (int s = 0; s < kN; ++s) {
+      barrier_init(full + 8 * s, 1);
+      barrier_init(ready + 8 * s, 2 * kGroupWarps + (kTma ? 2 : 0));
+      barrier_init(empty + 8 * s, 1);
     }
-    for (int s = 0; s < kB; ++s) {
-      barrier_init(ready_b + 8 * s, 2 * kGroupWarps);
-      barrier_init(empty_b + 8 * s, 1);
-    }
-    for (int s = 0; s < kStagesC; ++s) {
-      barrier_init(full_c + 8 * s, 1);
-      barrier_init(empty_c + 8 * s, kGroupWarps);
+    for (int s = 0; s < kCodeStages; ++s) {
+      barrier_init(code_full + 8 * s, 1);
+      barrier_init(code_empty + 8 * s, kGroupWarps);
     }
     for (int i = 0; i < 2; ++i) {
       barrier_init(acc_full + 8 * i, 1);
@@ -306,101 +312,105 @@ act_wgrad_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_consta
 
   if (warp < kFirstEpilogue) {
     fewer_registers<kIssueRegs>();
-    if (warp == 0 && lane == 0) {
+    if (warp == 0) {
       // copies
-      Ring<kA> ra = {0, 0};
-      Ring<kStagesC> rc = {0, 0};
+      const bool one = elect_one();
+      Ring<kN> r = {0, 0};
+      Ring<kCodeStages> rc = {0, 0};
       uint32_t issued = 0;
       bool ok = true;
       for (uint32_t u = pair; u < plan.units && ok; u += pairs) {
         const TileWork w = unit_of(plan, u);
         const int n = static_cast<int>(w.n0 + rank * kWgHalf), k = static_cast<int>(w.k0 + rank * kWgHalf);
         for (uint32_t y = static_cast<uint32_t>(w.row0); y < static_cast<uint32_t>(w.row1); y += kWgRows) {
-          if (!(ok = barrier_wait(empty_c + 8 * rc.at, rc.phase ^ 1u, &gave_up))) break;
-          const uint32_t bar_c = full_c + 8 * rc.at, c = at_c + rc.at * kCodeStage;
-          barrier_expect(bar_c, kCodeStage);
-          tma_load(c, &map_codes, k, y, bar_c);
-          tma_load(c + kCodeBytes, &map_exps, (k / kActBlock) & ~15, y, bar_c);
+          if (!(ok = all_wait(code_empty + 8 * rc.at, rc.phase ^ 1u, &gave_up))) break;
+          if (one) {
+            const uint32_t bar = code_full + 8 * rc.at, at = at_codes + rc.at * kCodeStage;
+            barrier_expect(bar, kCodeStage);
+            tma_load(at, &map_codes, k, y, bar);
+            tma_load(at + kCodeBytes, &map_exps, (k / kActBlock) & ~15, y, bar);
+          }
           rc.next();
           if (kTma) {
-            if (!(ok = barrier_wait(empty_a + 8 * ra.at, ra.phase ^ 1u, &gave_up))) break;
-            const uint32_t bar_a = full_a + 8 * ra.at, at = at_a + ra.at * kStageA;
-            barrier_expect(bar_a, kOperandBytes);
-            tma_load(at, &map_dy, n, y, bar_a);
-            tma_load(at + kAtomBytes, &map_dy, n + 64, y, bar_a);
-            ra.next();
+            if (!(ok = all_wait(empty + 8 * r.at, r.phase ^ 1u, &gave_up))) break;
+            if (one) {
+              const uint32_t bar = full + 8 * r.at, at = at_ring + r.at * kStage;
+              barrier_expect(bar, kOperandBytes);
+              tma_load(at, &map_dy, n, y, bar);
+              tma_load(at + kAtomBytes, &map_dy, n + 64, y, bar);
+            }
+            r.next();
           }
           ++issued;
         }
       }
       if (!ok) {  // gave up: the copies in flight land before the CTA leaves
-        for (uint32_t i = min(issued + 1, static_cast<uint32_t>(kStagesC)); i > 0; --i) {
+        for (uint32_t i = min(issued + 1, static_cast<uint32_t>(kCodeStages)); i > 0; --i) {
           rc.back();
-          barrier_drain(full_c + 8 * rc.at, rc.phase);
+          barrier_drain(code_full + 8 * rc.at, rc.phase);
         }
-        for (uint32_t i = kTma ? min(issued, static_cast<uint32_t>(kA)) : 0; i > 0; --i) {
-          ra.back();
-          barrier_drain(full_a + 8 * ra.at, ra.phase);
+        for (uint32_t i = kTma ? min(issued, static_cast<uint32_t>(kN)) : 0; i > 0; --i) {
+          r.back();
+          barrier_drain(full + 8 * r.at, r.phase);
         }
       }
-    } else if (warp == 1 && lane == 0) {
-      Ring<kA> ra = {0, 0};
-      Ring<kB> rb = {0, 0};
+    } else if (warp == 1) {
+      // products
+      const bool one = elect_one();
+      const uint32_t desc0 = desc_low(at_ring);
+      Ring<kN> r = {0, 0};
       Ring<2> acc = {0, 0};
       bool ok = true;
       for (uint32_t u = pair; u < plan.units && ok; u += pairs) {
         const TileWork w = unit_of(plan, u);
         uint32_t left = static_cast<uint32_t>((w.row1 - w.row0 + kWgRows - 1) / kWgRows);
+        if (rank != 0) {  // the first CTA issues; this one keeps count of the ring
+          for (; left; --left) r.next();
+          continue;
+        }
         while (left && ok) {
-          const uint32_t stages = min(left, static_cast<uint32_t>(kSegment));
+          const uint32_t stages = min(left, static_cast<uint32_t>(kSegment)), to = tmem + acc.at * kWgTile;
           left -= stages;
-          if (rank == 0) {  // products
-            if (!(ok = barrier_wait(acc_empty + 8 * acc.at, acc.phase ^ 1u, &gave_up))) break;
-            bool add = false;
-            for (uint32_t i = 0; i < stages; ++i) {
-              if (!(ok = barrier_wait(ready_b + 8 * rb.at, rb.phase, &gave_up))) break;
-              if (!(ok = barrier_wait(ready_a + 8 * ra.at, ra.phase, &gave_up))) break;
-              asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-              const uint32_t pa = at_a + ra.at * kStageA, pb = at_b + rb.at * kOperandBytes;
+          if (!(ok = all_wait(acc_empty + 8 * acc.at, acc.phase ^ 1u, &gave_up))) break;
+          for (uint32_t i = 0; i < stages; ++i) {
+            if (!(ok = all_wait(ready + 8 * r.at, r.phase, &gave_up))) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const uint32_t da = desc0 + r.at * (kStage >> 4), db = da + kP * (kOperandBytes >> 4);
+            if (one) {
 #pragma unroll
-              for (int j = 0; j < kWgRows / 16; ++j) {
-                const uint64_t b = operand_desc(pb + j * 2048);
+              for (int j = 0; j < kWgRows / 16; ++j)
 #pragma unroll
-                for (int p = 0; p < kP; ++p) {
-                  mma_pair(tmem + acc.at * kWgTile, operand_desc(pa + p * kOperandBytes + j * 2048), b, add);
-                  add = true;
-                }
-              }
-              mma_commit(empty_a + 8 * ra.at);
-              mma_commit(empty_b + 8 * rb.at);
-              ra.next(), rb.next();
+                for (int p = 0; p < kP; ++p)
+                  mma_pair(to, da + p * (kOperandBytes >> 4) + j * (2048 >> 4), db + j * (2048 >> 4), j || p ? 1u : i);
+              mma_commit(empty + 8 * r.at);
             }
-            mma_commit(acc_full + 8 * acc.at);
-            if (!ok) barrier_drain(acc_full + 8 * acc.at, acc.phase);  // gave up: the products in flight end first
-            acc.next();
-          } else {
-            for (uint32_t i = 0; i < stages; ++i) ra.next(), rb.next();
+            __syncwarp();
+            r.next();
           }
+          if (one) mma_commit(acc_full + 8 * acc.at);
+          __syncwarp();
+          if (!ok) barrier_drain(acc_full + 8 * acc.at, acc.phase);  // gave up: the products in flight end first
+          acc.next();
         }
       }
-      last_a = ra, last_b = rb;
+      if (lane == 0) last_at = r.at, last_phase = r.phase;
     } else if (warp == 3 && kTma) {
-      Ring<kA> ra = {0, 0};
-      const uint32_t ready_of_first = map_rank(ready_a, 0);
+      Ring<kN> r = {0, 0};
+      const uint32_t ready_of_first = map_rank(ready, 0);
       bool ok = true;
       for (uint32_t u = pair; u < plan.units && ok; u += pairs) {
         const TileWork w = unit_of(plan, u);
         uint32_t rows = static_cast<uint32_t>(w.row1 - w.row0);
         while (rows) {
-          if (!(ok = __all_sync(0xffffffffu, barrier_wait(full_a + 8 * ra.at, ra.phase, &gave_up)))) break;
+          if (!(ok = all_wait(full + 8 * r.at, r.phase, &gave_up))) break;
           if (rows < kWgRows) {  // rows of another worker came with the copy: they must not meet 0 * inf
             for (uint32_t i = lane; i < (kWgRows - rows) * 16; i += 32)
-              store_shared(at_a + ra.at * kStageA + chunk_offset(rows + (i >> 4), i & 15u), make_uint4(0u, 0u, 0u, 0u));
+              store_shared(at_ring + r.at * kStage + chunk_offset(rows + (i >> 4), i & 15u), make_uint4(0u, 0u, 0u, 0u));
           }
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
-          if (lane == 0) barrier_arrive_cluster(ready_of_first + 8 * ra.at);
-          ra.next();
+          if (lane == 0) barrier_arrive_cluster(ready_of_first + 8 * r.at);
+          r.next();
           rows -= min(rows, static_cast<uint32_t>(kWgRows));
         }
       }
@@ -410,60 +420,61 @@ act_wgrad_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_consta
     fewer_registers<kConvertRegs>();
     constexpr int kLoads = sizeof(T) == 4 ? 2 : 4;  // chunks of dy a thread has in flight
     const uint32_t group = (warp - kFirstConvert) / kGroupWarps, ctid = tid - (kFirstConvert + group * kGroupWarps) * 32;
-    const uint32_t seg = ctid & 7u, chunk = ctid & 15u;
+    const uint32_t chunk = ctid & 15u;
+    // a thread takes eight columns (seg) of either atom in rows r0, r0 + 16, ...; threads of odd rows take the
+    // second atom first, so that 16 threads' loads cover all banks
+    const uint32_t seg = ctid & 7u, r0 = ctid >> 3, second = r0 & 1u;
+    const uint32_t from0 = r0 * kWgHalf + second * 64 + seg * 8, from1 = from0 ^ 64u;
+    const uint32_t to0 = chunk_offset(r0, second * 8 + seg), to1 = to0 ^ kAtomBytes;
+    const uint32_t byte0 = 0x4440u + second * 2 + (seg >> 2), byte1 = byte0 ^ 2u;  // their exponent bytes in a row's word
     const T* dy = static_cast<const T*>(a.dy);
-    const uint32_t ready_a_first = map_rank(ready_a, 0), ready_b_first = map_rank(ready_b, 0);
-    Ring<kA> ra = {0, 0};
-    Ring<kB> rb = {0, 0};
-    Ring<kStagesC> rc = {0, 0};
+    const uint32_t ready_of_first = map_rank(ready, 0), code_empty_own = map_rank(code_empty, rank);
+    Ring<kN> r = {0, 0};
+    Ring<kCodeStages> rc = {0, 0};
     uint32_t turn = 0;
     bool ok = true;
     for (uint32_t u = pair; u < plan.units && ok; u += pairs) {
       const TileWork w = unit_of(plan, u);
-      const uint32_t exp_at = (((w.k0 + rank * kWgHalf) / kActBlock) & 15u) + (seg >> 1);
+      const uint32_t exp_at = ((w.k0 + rank * kWgHalf) / kActBlock) & 15u;  // four blocks: one word
       const uint32_t n = w.n0 + rank * kWgHalf + chunk * kUnit;
-      for (uint64_t t = w.row0; t < w.row1; t += kWgRows, ra.next(), rb.next(), rc.next(), turn ^= 1u) {
+      for (uint64_t t = w.row0; t < w.row1; t += kWgRows, r.next(), rc.next(), turn ^= 1u) {
         if (turn != group) continue;
         const uint32_t rows = static_cast<uint32_t>(min(static_cast<uint64_t>(kWgRows), w.row1 - t));
         Unit<T> raw[kTma ? 1 : kLoads];
         auto load = [&](int batch) {
 #pragma unroll
           for (int i = 0; i < kLoads; ++i) {
-            const uint32_t r = (ctid >> 4) + 8 * (batch * kLoads + i);
-            raw[kTma ? 0 : i] = load_raw<T>(dy + (t + r) * a.ld_dy, n, r < rows ? a.out_cols : 0u);
+            const uint32_t y = (ctid >> 4) + 8 * (batch * kLoads + i);
+            raw[kTma ? 0 : i] = load_raw<T>(dy + (t + y) * a.ld_dy, n, y < rows ? a.out_cols : 0u);
           }
         };
         if (!kTma) load(0);
-        if (!(ok = __all_sync(0xffffffffu, barrier_wait(full_c + 8 * rc.at, rc.phase, &gave_up)))) break;
-        if (!(ok = __all_sync(0xffffffffu, barrier_wait(empty_b + 8 * rb.at, rb.phase ^ 1u, &gave_up)))) break;
-        const uint32_t codes = at_c + rc.at * kCodeStage, out = at_b + rb.at * kOperandBytes;
-        uint4 c[4];
-        uint32_t b[4];
+        if (!(ok = all_wait(code_full + 8 * rc.at, rc.phase, &gave_up))) break;
+        if (!(ok = all_wait(empty + 8 * r.at, r.phase ^ 1u, &gave_up))) break;
+        const uint32_t codes = at_codes + rc.at * kCodeStage, stage = at_ring + r.at * kStage, out = stage + kP * kOperandBytes;
+        uint2 c0[4], c1[4];
+        uint32_t e[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const uint32_t r = (ctid >> 3) + 16 * i;
-          c[i] = load_shared(codes + r * kWgHalf + seg * 16);
-          b[i] = load_shared_byte(codes + kCodeBytes + r * 16 + exp_at);
+          c0[i] = load_shared2(codes + from0 + i * 16 * kWgHalf);
+          c1[i] = load_shared2(codes + from1 + i * 16 * kWgHalf);
+          e[i] = load_shared1(codes + kCodeBytes + (r0 + 16 * i) * 16 + exp_at);
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const uint32_t r = (ctid >> 3) + 16 * i;
-          const uint32_t unit = b[i] == kActNan ? 0x7fffu : (b[i] - 6u) << 7, unit2 = unit | (unit << 16);
-          uint4 lo = code_octet(c[i].x, c[i].y, unit2), hi = code_octet(c[i].z, c[i].w, unit2);
-          if (r >= rows) lo = hi = make_uint4(0u, 0u, 0u, 0u);
-          // segments of the second atom store their odd chunk first: eight threads then cover all banks
-          const bool odd_first = seg >= 4;
-          store_shared(out + chunk_offset(r, 2 * seg + (odd_first ? 1 : 0)), odd_first ? hi : lo);
-          store_shared(out + chunk_offset(r, 2 * seg + (odd_first ? 0 : 1)), odd_first ? lo : hi);
+          store_shared(out + to0 + i * 2048, code_octet(c0[i], __byte_perm(e[i], 0u, byte0) * 0x00800080u));
+          store_shared(out + to1 + i * 2048, code_octet(c1[i], __byte_perm(e[i], 0u, byte1) * 0x00800080u));
         }
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        __syncwarp();
-        if (lane == 0) {
-          barrier_arrive_cluster(empty_c + 8 * rc.at);
-          barrier_arrive_cluster(ready_b_first + 8 * rb.at);
+        if (rows < kWgRows) {  // rows past the worker's: no row of its own stands there yet
+          __syncwarp();
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (r0 + 16 * i >= rows) {
+              store_shared(out + to0 + i * 2048, make_uint4(0u, 0u, 0u, 0u));
+              store_shared(out + to1 + i * 2048, make_uint4(0u, 0u, 0u, 0u));
+            }
         }
         if (!kTma) {
-          if (!(ok = __all_sync(0xffffffffu, barrier_wait(empty_a + 8 * ra.at, ra.phase ^ 1u, &gave_up)))) break;
           for (int batch = 0; batch < 8 / kLoads; ++batch) {
             if (batch) load(batch);
 #pragma unroll
@@ -481,14 +492,17 @@ act_wgrad_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_consta
                   const float rest = v[j] - __uint_as_float(__float_as_uint(v[j]) & 0xffff0000u);
                   v[j] = fabsf(v[j]) < INFINITY ? rest : 0.f;
                 }
-                store_shared(at_a + ra.at * kStageA + p * kOperandBytes + chunk_offset((ctid >> 4) + 8 * (batch * kLoads + i), chunk),
+                store_shared(stage + p * kOperandBytes + chunk_offset((ctid >> 4) + 8 * (batch * kLoads + i), chunk),
                              make_uint4(q[0], q[1], q[2], q[3]));
               }
             }
           }
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-          __syncwarp();
-          if (lane == 0) barrier_arrive_cluster(ready_a_first + 8 * ra.at);
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) {
+          barrier_arrive_cluster(code_empty_own + 8 * rc.at);
+          barrier_arrive_cluster(ready_of_first + 8 * r.at);
         }
       }
     }
@@ -508,7 +522,7 @@ act_wgrad_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_consta
       for (int i = 0; i < kWgHalf; ++i) sum[i] = 0.f;
       for (uint32_t left = static_cast<uint32_t>((w.row1 - w.row0 + kWgRows - 1) / kWgRows); left;
            left -= min(left, static_cast<uint32_t>(kSegment))) {
-        if (!(ok = __all_sync(0xffffffffu, barrier_wait(acc_full + 8 * acc.at, acc.phase, &gave_up)))) break;
+        if (!(ok = all_wait(acc_full + 8 * acc.at, acc.phase, &gave_up))) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const uint32_t from = tmem + acc.at * kWgTile + half * kWgHalf + (quarter << 21);
 #pragma unroll
@@ -530,7 +544,7 @@ act_wgrad_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_consta
       for (int c = 0; c < kWgHalf; c += kTurnCols) {
         __syncwarp();
 #pragma unroll
-        for (int i = 0; i < kTurnCols; ++i) turn[lane * kTurnPitch + i] = sum[c + i];
+        for (int i = 0; i < kTurnCols; ++i) turn[lane * kTurnPitch + product_column(i)] = sum[c + i];
         __syncwarp();
         const float* from = turn + (lane >> 4) * kTurnPitch + (lane & 15u);
         const uint32_t k = w.k0 + col + c, n = w.n0 + row;
@@ -558,8 +572,8 @@ act_wgrad_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_consta
   __syncthreads();
   if (tid == 32) {  // the arrivals that release the last stages land before the CTA leaves
     bool ok = !gave_up;
-    for (int i = 0; i < kA && ok; ++i, last_a.next()) ok = barrier_wait(empty_a + 8 * last_a.at, last_a.phase ^ 1u, &gave_up);
-    for (int i = 0; i < kB && ok; ++i, last_b.next()) ok = barrier_wait(empty_b + 8 * last_b.at, last_b.phase ^ 1u, &gave_up);
+    Ring<kN> r = {last_at, last_phase};
+    for (int i = 0; i < kN && ok; ++i, r.next()) ok = barrier_wait(empty + 8 * r.at, r.phase ^ 1u, &gave_up);
   }
   __syncwarp();
   cluster_sync();
