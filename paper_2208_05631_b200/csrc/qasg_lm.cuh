@@ -64,6 +64,16 @@ template <> __device__ __forceinline__ void unit_floats<float>(const Unit<float>
   for (int i = 0; i < kUnit; ++i) v[i] = __uint_as_float(u.w[i]);
 }
 
+__device__ __forceinline__ __nv_bfloat162 pair_of(__nv_bfloat16 v) { return __nv_bfloat162(v, v); }
+__device__ __forceinline__ __half2 pair_of(__half v) { return __half2(v, v); }
+// Puts a value that the type holds at place k of a unit.
+template <typename T> __device__ __forceinline__ void set_value(Unit<T>& u, int k, float v) {
+  const T t = from_float<T>(v);
+  const uint32_t b = *reinterpret_cast<const uint16_t*>(&t);
+  u.w[k / 2] = k & 1 ? u.w[k / 2] | (b << 16) : b;  // places are set in rising order
+}
+template <> __device__ __forceinline__ void set_value<float>(Unit<float>& u, int k, float v) { u.w[k] = __float_as_uint(v); }
+
 // Values [i, i + 8) of a row of n values, `fill` outside the row; any alignment of the row.
 template <typename T>
 __device__ __forceinline__ void load_values(const T* row, int64_t i, int64_t n, float fill, float (&v)[kUnit]) {

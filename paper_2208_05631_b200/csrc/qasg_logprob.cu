@@ -3,8 +3,10 @@
 //   dx_v = p_v (g_lse - g_logprob - g_entropy (log p_v + entropy)) + [v = token] g_logprob.
 // Forward: one pass over the logits.  A thread keeps the running maximum m, s = sum 2^y and t = sum y 2^y with
 // y = (x - m) log2(e); when m grows by d (in units of log2), s becomes 2^-d s and t becomes 2^-d (t - d s).
-// Alternatives: a candidate is an element at least as large as a lower bound of the k-th largest value seen so
-// far; candidates go to a short list in shared memory that is cut back to its k best, which raises the bound.
+// Alternatives: a candidate is an element at least as large as a lower bound of the k-th largest value; candidates
+// go to a list in shared memory.  The bound comes from the first round of loads (its exact k-th largest element,
+// found by cutting that round's candidates back to k); after it the warps of a CTA do not meet until the row
+// ends.  A row with more candidates than the list holds (rising values, ties) is scanned again for them alone.
 // A row is shared by the CTAs of a cluster where there are fewer rows than the GPU has room for.
 #include <cooperative_groups.h>
 
@@ -15,8 +17,8 @@ namespace cg = cooperative_groups;
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kTiny = -160.f;  // 2^kTiny is 0 in fp32: stands for every smaller power, so that 0 * y is 0
-constexpr int kRowUnits = 4;     // units a thread loads per round
-constexpr int kListSize = 1024;  // candidates kept before they are cut back to the k best
+template <typename T> constexpr int kRoundUnits = sizeof(T) == 4 ? 2 : 4;  // units a thread loads per round: 64 bytes
+constexpr int kListSize = 1024;  // candidates a CTA has room for
 constexpr int kMaxCluster = 8;
 
 __device__ __forceinline__ float exp2_fast(float y) {
@@ -37,6 +39,31 @@ __device__ __forceinline__ unsigned long long value_key(float x, uint32_t column
 __device__ __forceinline__ float key_value(unsigned long long key) {
   const uint32_t o = static_cast<uint32_t>(key >> 32);
   return __uint_as_float(o == 0xffffffffu ? 0x7fffffffu : (o >> 31) ? (o ^ 0x80000000u) : ~o);
+}
+
+// A unit of row values [i, i + 8) of n, -inf outside the row.
+template <typename T> __device__ __forceinline__ Unit<T> load_row_unit(const T* row, int64_t i, int64_t n) {
+  if (i >= 0 && i + kUnit <= n) return load_unit(row + i);  // the caller's units lie on 16-byte boundaries
+  Unit<T> u;
+#pragma unroll
+  for (int k = 0; k < kUnit; ++k) {
+    const float v = i + k >= 0 && i + k < n ? to_float(row[i + k]) : -INFINITY;
+    set_value(u, k, v);
+  }
+  return u;
+}
+template <typename T> __device__ __forceinline__ float unit_top(const Unit<T>& u) {
+  typedef decltype(pair_of(T())) Pair;
+  Pair m = *reinterpret_cast<const Pair*>(&u.w[0]);
+#pragma unroll
+  for (int i = 1; i < kUnit / 2; ++i) m = __hmax2_nan(m, *reinterpret_cast<const Pair*>(&u.w[i]));
+  return max_nan(to_float(m.x), to_float(m.y));
+}
+template <> __device__ __forceinline__ float unit_top<float>(const Unit<float>& u) {
+  float m = __uint_as_float(u.w[0]);
+#pragma unroll
+  for (int i = 1; i < kUnit; ++i) m = max_nan(m, __uint_as_float(u.w[i]));
+  return m;
 }
 
 struct RowSums {
@@ -60,7 +87,7 @@ struct RowShared {
   float group_max[32];
   RowSums warp_sums[32];
   RowSums sums;
-  unsigned int count;
+  unsigned int count, lost;
   unsigned long long bound;
 };
 
@@ -86,9 +113,38 @@ __device__ __forceinline__ void cut_list(RowShared& sh, uint32_t k) {
   __syncthreads();
 }
 
+// Puts the candidates among a thread's units (pending: a bit for each element still to be looked at) on the list;
+// returns the bits of those that found no room.
+template <typename T, int kThreads>
+__device__ __forceinline__ uint32_t push_pending(RowShared& sh, const T* x, uint32_t pending, int64_t c0) {
+  const unsigned long long limit = sh.bound;
+  uint32_t left = 0;
+  while (pending) {
+    const int b = __ffs(pending) - 1;
+    pending &= pending - 1;
+    const uint32_t c = static_cast<uint32_t>(c0 + static_cast<int64_t>(b >> 3) * (kThreads * kUnit) + (b & 7));
+    const unsigned long long key = value_key(to_float(x[c]), c);
+    if (key < limit) continue;
+    const uint32_t at = atomicAdd(&sh.count, 1u);
+    if (at < kListSize) sh.list[at] = key;
+    else left |= 1u << b;
+  }
+  return left;
+}
+
+// One round of units at which all warps meet, so that the list is cut back as often as it fills up.
+template <typename T, int kThreads>
+__device__ __noinline__ void push_round(RowShared& sh, const T* x, uint32_t k, uint32_t pending, int64_t c0) {
+  do {
+    pending = push_pending<T, kThreads>(sh, x, pending, c0);
+    cut_list<kThreads>(sh, k);
+  } while (__syncthreads_or(pending != 0));
+}
+
 template <typename T, int kThreads, bool kTop>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, 1024 / kThreads)
 token_logprob_kernel(LogprobArgs a, uint32_t cluster, unsigned int* __restrict__ status) {
+  constexpr int kUnits = kRoundUnits<T>;
   __shared__ RowShared sh;
   const uint64_t row = blockIdx.x / cluster;
   const uint32_t part = blockIdx.x - static_cast<uint32_t>(row) * cluster, tid = threadIdx.x, vocab = a.vocab;
@@ -114,11 +170,7 @@ token_logprob_kernel(LogprobArgs a, uint32_t cluster, unsigned int* __restrict__
       return;
     }
   }
-  const float given = to_float(x[token]);
-  if (kTop) {
-    if (tid == 0) sh.count = 0, sh.bound = 0;
-    __syncthreads();
-  }
+  if (kTop && tid == 0) sh.count = 0, sh.lost = 0, sh.bound = 0;
   // units on 16-byte boundaries: unit u holds columns 8u - off .. 8u - off + 7
   const uint32_t off = static_cast<uint32_t>((reinterpret_cast<uintptr_t>(x) & 15u) / sizeof(T));
   const uint32_t units = (vocab + off + kUnit - 1) / kUnit, per_part = (units + cluster - 1) / cluster;
@@ -126,20 +178,20 @@ token_logprob_kernel(LogprobArgs a, uint32_t cluster, unsigned int* __restrict__
   RowSums r = {-INFINITY, 0.f, 0.f};
   float base = 0.f;  // m, 0 while m is -inf
   float bound = -INFINITY;
-  for (uint32_t u = u0; u < u1; u += kThreads * kRowUnits) {
-    float v[kRowUnits][kUnit], top[kRowUnits];
+  for (uint32_t u = u0; u < u1; u += kThreads * kUnits) {
+    Unit<T> raw[kUnits];
+    float top[kUnits];
 #pragma unroll
-    for (int j = 0; j < kRowUnits; ++j) {
+    for (int j = 0; j < kUnits; ++j) {
       const uint32_t w = u + j * kThreads + tid;
-      load_values<T>(x, static_cast<int64_t>(w) * kUnit - off, w < u1 ? vocab : 0, -INFINITY, v[j]);
+      raw[j] = load_row_unit<T>(x, static_cast<int64_t>(w) * kUnit - off, w < u1 ? vocab : 0);
     }
+    float m = -INFINITY;
 #pragma unroll
-    for (int j = 0; j < kRowUnits; ++j) {
-      top[j] = v[j][0];
-#pragma unroll
-      for (int k = 1; k < kUnit; ++k) top[j] = max_nan(top[j], v[j][k]);
+    for (int j = 0; j < kUnits; ++j) {
+      top[j] = unit_top(raw[j]);
+      m = max_nan(m, top[j]);
     }
-    const float m = max_nan(max_nan(top[0], top[1]), max_nan(top[2], top[3]));
     if (!(m <= r.m)) {
       const float d = max_nan((r.m - m) * kLog2e, kTiny), c = exp2_fast(d);
       r.t = c * fmaf(r.s, d, r.t);
@@ -147,72 +199,87 @@ token_logprob_kernel(LogprobArgs a, uint32_t cluster, unsigned int* __restrict__
       r.m = m;
       base = m;
     }
-#pragma unroll
-    for (int j = 0; j < kRowUnits; ++j)
-#pragma unroll
-      for (int k = 0; k < kUnit; ++k) {
-        const float y = max_nan((v[j][k] - base) * kLog2e, kTiny), e = exp2_fast(y);
-        r.s += e;
-        r.t = fmaf(e, y, r.t);
-      }
     if (kTop) {
+      const int64_t c0 = static_cast<int64_t>(u + tid) * kUnit - off;
       if (u == u0) {
-        // 32 groups of threads hold distinct elements: the smallest of the groups' largest is at most the
-        // 32nd largest element, so at most the k-th largest
+        // The smallest of the largest elements of g groups is at most the g-th largest element of all, so with
+        // g >= k at most the k-th: g groups of threads, g the power of two from k on (up to 32).
         constexpr int kLanes = kThreads / 32;
-        float g = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+        float g = m == m ? m : INFINITY;
 #pragma unroll
         for (int s = kLanes / 2; s > 0; s >>= 1) g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, s));
         if (tid % kLanes == 0) sh.group_max[tid / kLanes] = g;
         __syncthreads();
         g = sh.group_max[tid & 31];
-#pragma unroll
-        for (int s = 16; s > 0; s >>= 1) g = fminf(g, __shfl_xor_sync(0xffffffffu, g, s));
-        bound = g;
+        const uint32_t wide = 32u >> (32 - __clz(a.k - 1));  // of the 32 groups of kLanes threads in one of the g
+        for (uint32_t s = 1; s < 32; s <<= 1) {
+          const float o = __shfl_xor_sync(0xffffffffu, g, s);
+          g = s < wide ? fmaxf(g, o) : fminf(g, o);
+        }
         if (tid == 0) sh.bound = static_cast<unsigned long long>(value_order(g)) << 32;
+        bound = g;
         __syncthreads();
       }
-      uint32_t pending = 0;  // elements the full list had no room for
-      bool crowded = false;
+      uint32_t pending = 0;
 #pragma unroll
-      for (int j = 0; j < kRowUnits; ++j) {
-        if (top[j] < bound) continue;
-        const unsigned long long limit = sh.bound;
-        const int64_t c0 = static_cast<int64_t>(u + j * kThreads + tid) * kUnit - off;
+      for (int j = 0; j < kUnits; ++j)
+        if (!(top[j] < bound)) {
+          const uint32_t w = u + j * kThreads + tid;
+          float v[kUnit];
+          unit_floats(raw[j], v);
 #pragma unroll
-        for (int k = 0; k < kUnit; ++k) {
-          if (v[j][k] < bound || c0 + k < 0 || c0 + k >= vocab || u + j * kThreads + tid >= u1) continue;
-          const unsigned long long key = value_key(v[j][k], static_cast<uint32_t>(c0 + k));
-          if (key < limit) continue;
-          const uint32_t at = atomicAdd(&sh.count, 1u);
-          if (at < kListSize) sh.list[at] = key;
-          else pending |= 1u << (j * kUnit + k);
-          crowded |= at >= kListSize / 2;
-        }
-      }
-      if (__syncthreads_or(crowded) || u == u0) {
-        cut_list<kThreads>(sh, a.k);
-        while (__syncthreads_or(pending != 0)) {
-          const unsigned long long limit = sh.bound;
-          for (uint32_t left = pending; left;) {
-            const int b = __ffs(left) - 1;
-            left &= left - 1;
-            const uint32_t c = static_cast<uint32_t>(static_cast<int64_t>(u + (b >> 3) * kThreads + tid) * kUnit - off + (b & 7));
-            const unsigned long long key = value_key(to_float(x[c]), c);
-            if (key >= limit) {
-              const uint32_t at = atomicAdd(&sh.count, 1u);
-              if (at >= kListSize) continue;  // stays pending
-              sh.list[at] = key;
-            }
-            pending &= ~(1u << b);
+          for (int k = 0; k < kUnit; ++k) {
+            const int64_t c = static_cast<int64_t>(w) * kUnit - off + k;
+            if (!(v[k] < bound) && w < u1 && c >= 0 && c < vocab) pending |= 1u << (j * kUnit + k);
           }
-          cut_list<kThreads>(sh, a.k);
         }
+      if (u == u0) {
+        push_round<T, kThreads>(sh, x, a.k, pending, c0);
         bound = key_value(sh.bound);
         if (bound != bound) bound = INFINITY;  // k NaNs: nothing but another NaN passes
+      } else if (pending) {
+        if (push_pending<T, kThreads>(sh, x, pending, c0)) sh.lost = 1u;
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kUnits; ++j) {
+      float v[kUnit];
+      unit_floats(raw[j], v);
+#pragma unroll
+      for (int k = 0; k < kUnit; ++k) {
+        const float y = max_nan((v[k] - base) * kLog2e, kTiny), e = exp2_fast(y);
+        r.s += e;
+        r.t = fmaf(e, y, r.t);
       }
     }
   }
+  if (kTop) {
+    __syncthreads();
+    if (sh.lost) {
+      // the k-th best of what was kept is a far better bound: once more, from the start, meeting at every round
+      cut_list<kThreads>(sh, a.k);
+      if (tid == 0) sh.count = 0, sh.bound = sh.best[a.k - 1];
+      __syncthreads();
+      for (uint32_t u = u0; u < u1; u += kThreads * kUnits) {
+        const int64_t c0 = static_cast<int64_t>(u + tid) * kUnit - off;
+        uint32_t pending = 0;
+        const float limit = key_value(sh.bound);
+#pragma unroll
+        for (int j = 0; j < kUnits; ++j) {
+          const uint32_t w = u + j * kThreads + tid;
+          float v[kUnit];
+          unit_floats(load_row_unit<T>(x, static_cast<int64_t>(w) * kUnit - off, w < u1 ? vocab : 0), v);
+#pragma unroll
+          for (int k = 0; k < kUnit; ++k) {
+            const int64_t c = static_cast<int64_t>(w) * kUnit - off + k;
+            if (!(v[k] < limit) && w < u1 && c >= 0 && c < vocab) pending |= 1u << (j * kUnit + k);
+          }
+        }
+        push_round<T, kThreads>(sh, x, a.k, pending, c0);
+      }
+    }
+  }
+  const float given = to_float(x[token]);
   // join the threads, then the CTAs
 #pragma unroll
   for (int s = 16; s > 0; s >>= 1) {
@@ -262,7 +329,7 @@ token_logprob_kernel(LogprobArgs a, uint32_t cluster, unsigned int* __restrict__
 }
 
 // ------------------------------------------------------------------ gradient
-constexpr int kGradThreads = 256;
+constexpr int kGradThreads = 256, kGradUnits = 4;
 template <typename T>
 __global__ void __launch_bounds__(kGradThreads)
 token_logprob_grad_kernel(LogprobGradArgs a, uint32_t per_row, unsigned int* __restrict__ status) {
@@ -281,15 +348,15 @@ token_logprob_grad_kernel(LogprobGradArgs a, uint32_t per_row, unsigned int* __r
   // p (c0 - c1 y) with y = log2 p
   const float c0 = g_lse - g_lp - (a.g_entropy ? g_h * a.entropy[row] : 0.f), c1 = g_h * kLn2;
   const uint32_t off = static_cast<uint32_t>((reinterpret_cast<uintptr_t>(dx) & 15u) / sizeof(T));
-  const uint32_t u0 = part * (kGradThreads * kRowUnits) + threadIdx.x;
-  float v[kRowUnits][kUnit];
+  const uint32_t u0 = part * (kGradThreads * kGradUnits) + threadIdx.x;
+  float v[kGradUnits][kUnit];
   if (!zero) {
 #pragma unroll
-    for (int j = 0; j < kRowUnits; ++j)
+    for (int j = 0; j < kGradUnits; ++j)
       load_values<T>(x, static_cast<int64_t>(u0 + j * kGradThreads) * kUnit - off, vocab, -INFINITY, v[j]);
   }
 #pragma unroll
-  for (int j = 0; j < kRowUnits; ++j) {
+  for (int j = 0; j < kGradUnits; ++j) {
     const int64_t c = static_cast<int64_t>(u0 + j * kGradThreads) * kUnit - off;
 #pragma unroll
     for (int k = 0; k < kUnit; ++k) {
@@ -326,7 +393,7 @@ int launch_token_logprob(int dtype, const LogprobArgs& a, unsigned int* status, 
 int launch_token_logprob_grad(int dtype, const LogprobGradArgs& a, unsigned int* status, const LaunchShape& shape,
                               cudaStream_t stream) {
   // one unit more than the row's: it may begin inside a 16-byte group
-  const uint32_t per_row = (a.vocab / kUnit + 2 + kGradThreads * kRowUnits - 1) / (kGradThreads * kRowUnits);
+  const uint32_t per_row = (a.vocab / kUnit + 2 + kGradThreads * kGradUnits - 1) / (kGradThreads * kGradUnits);
   with_dtype(dtype, [&](auto t) {
     using T = decltype(t);
     launch_lm(token_logprob_grad_kernel<T>, dim3(static_cast<unsigned>(a.rows * per_row)), kGradThreads, 0, 1, stream,
