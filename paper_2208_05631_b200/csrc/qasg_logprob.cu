@@ -5,8 +5,8 @@
 // y = (x - m) log2(e); when m grows by d (in units of log2), s becomes 2^-d s and t becomes 2^-d (t - d s).
 // Alternatives: a candidate is an element at least as large as a lower bound of the k-th largest value; candidates
 // go to a list in shared memory.  The bound comes from the first round of loads (its exact k-th largest element,
-// found by cutting that round's candidates back to k); after it the warps of a CTA do not meet until the row
-// ends.  A row with more candidates than the list holds (rising values, ties) is scanned again for them alone.
+// found by cutting that round's candidates back to k), and again from rounds 4, 16, 64, ...; in between the warps
+// of a CTA do not meet.  A row with more candidates than the list holds (rising values, ties) is scanned again for them alone.
 // A row is shared by the CTAs of a cluster where there are fewer rows than the GPU has room for.
 #include <cooperative_groups.h>
 
@@ -21,9 +21,30 @@ template <typename T> constexpr int kRoundUnits = sizeof(T) == 4 ? 2 : 4;  // un
 constexpr int kListSize = 1024;  // candidates a CTA has room for
 constexpr int kMaxCluster = 8;
 
+// 2^y within 2 units in the last place; below 2^-126 it is 0.
 __device__ __forceinline__ float exp2_fast(float y) {
   float r;
-  asm("ex2.approx.f32 %0, %1;" : "=f"(r) : "f"(y));
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(y));
+  return r;
+}
+// Two fp32 operations in one instruction.
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 r;
+  asm("{\n.reg .b64 a, b, r;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nadd.rn.f32x2 r, a, b;\nmov.b64 {%0, %1}, r;\n}"
+      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return r;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 r;
+  asm("{\n.reg .b64 a, b, r;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nmul.rn.f32x2 r, a, b;\nmov.b64 {%0, %1}, r;\n}"
+      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return r;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 r;
+  asm("{\n.reg .b64 a, b, c, r;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nmov.b64 c, {%6, %7};\n"
+      "fma.rn.f32x2 r, a, b, c;\nmov.b64 {%0, %1}, r;\n}"
+      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
   return r;
 }
 
@@ -176,16 +197,20 @@ token_logprob_kernel(LogprobArgs a, uint32_t cluster, unsigned int* __restrict__
   const uint32_t units = (vocab + off + kUnit - 1) / kUnit, per_part = (units + cluster - 1) / cluster;
   const uint32_t u0 = part * per_part, u1 = min(units, u0 + per_part);
   RowSums r = {-INFINITY, 0.f, 0.f};
-  float base = 0.f;  // m, 0 while m is -inf
+  float2 s2 = {0.f, 0.f}, t2 = {0.f, 0.f};  // s and t of the even and the odd columns
+  float base = 0.f;                         // m, 0 while m is -inf
   float bound = -INFINITY;
-  for (uint32_t u = u0; u < u1; u += kThreads * kUnits) {
+  uint32_t meet = u0;  // the next round at which the list is cut back: 0, 4, 16, 64, ...
+  // One round of units from u on; inside: every unit lies in this part and inside the row.
+  auto round = [&](uint32_t u, auto inside) {
+    constexpr bool kInside = decltype(inside)::value;
+    const int64_t c0 = static_cast<int64_t>(u + tid) * kUnit - off;
     Unit<T> raw[kUnits];
     float top[kUnits];
 #pragma unroll
-    for (int j = 0; j < kUnits; ++j) {
-      const uint32_t w = u + j * kThreads + tid;
-      raw[j] = load_row_unit<T>(x, static_cast<int64_t>(w) * kUnit - off, w < u1 ? vocab : 0);
-    }
+    for (int j = 0; j < kUnits; ++j)
+      raw[j] = kInside ? load_unit(x + c0 + j * kThreads * kUnit)
+                       : load_row_unit<T>(x, c0 + j * kThreads * kUnit, u + j * kThreads + tid < u1 ? vocab : 0);
     float m = -INFINITY;
 #pragma unroll
     for (int j = 0; j < kUnits; ++j) {
@@ -194,13 +219,12 @@ token_logprob_kernel(LogprobArgs a, uint32_t cluster, unsigned int* __restrict__
     }
     if (!(m <= r.m)) {
       const float d = max_nan((r.m - m) * kLog2e, kTiny), c = exp2_fast(d);
-      r.t = c * fmaf(r.s, d, r.t);
-      r.s *= c;
+      t2 = mul2(make_float2(c, c), fma2(s2, make_float2(d, d), t2));
+      s2 = mul2(make_float2(c, c), s2);
       r.m = m;
       base = m;
     }
     if (kTop) {
-      const int64_t c0 = static_cast<int64_t>(u + tid) * kUnit - off;
       if (u == u0) {
         // The smallest of the largest elements of g groups is at most the g-th largest element of all, so with
         // g >= k at most the k-th: g groups of threads, g the power of two from k on (up to 32).
@@ -221,20 +245,27 @@ token_logprob_kernel(LogprobArgs a, uint32_t cluster, unsigned int* __restrict__
         __syncthreads();
       }
       uint32_t pending = 0;
+      if (!(m < bound)) {
 #pragma unroll
-      for (int j = 0; j < kUnits; ++j)
-        if (!(top[j] < bound)) {
-          const uint32_t w = u + j * kThreads + tid;
-          float v[kUnit];
-          unit_floats(raw[j], v);
+        for (int j = 0; j < kUnits; ++j)
+          if (!(top[j] < bound)) {
+            float v[kUnit];
+            unit_floats(raw[j], v);
+            uint32_t bits = 0;
 #pragma unroll
-          for (int k = 0; k < kUnit; ++k) {
-            const int64_t c = static_cast<int64_t>(w) * kUnit - off + k;
-            if (!(v[k] < bound) && w < u1 && c >= 0 && c < vocab) pending |= 1u << (j * kUnit + k);
+            for (int k = 0; k < kUnit; ++k) bits |= v[k] < bound ? 0u : 1u << k;
+            if (!kInside) {  // not what lies outside the row, or in another part
+              const int64_t c = c0 + j * kThreads * kUnit;
+              if (c < 0) bits &= 0xffu << -c;
+              if (c + kUnit > vocab) bits &= c >= vocab ? 0u : 0xffu >> (c + kUnit - vocab);
+              if (u + j * kThreads + tid >= u1) bits = 0u;
+            }
+            pending |= bits << (j * kUnit);
           }
-        }
-      if (u == u0) {
+      }
+      if (u == meet) {
         push_round<T, kThreads>(sh, x, a.k, pending, c0);
+        meet = u0 + max(4u * (u - u0), 4u * kThreads * kUnits);
         bound = key_value(sh.bound);
         if (bound != bound) bound = INFINITY;  // k NaNs: nothing but another NaN passes
       } else if (pending) {
@@ -246,13 +277,21 @@ token_logprob_kernel(LogprobArgs a, uint32_t cluster, unsigned int* __restrict__
       float v[kUnit];
       unit_floats(raw[j], v);
 #pragma unroll
-      for (int k = 0; k < kUnit; ++k) {
-        const float y = max_nan((v[k] - base) * kLog2e, kTiny), e = exp2_fast(y);
-        r.s += e;
-        r.t = fmaf(e, y, r.t);
+      for (int k = 0; k < kUnit; k += 2) {
+        float2 y = mul2(add2(make_float2(v[k], v[k + 1]), make_float2(-base, -base)), make_float2(kLog2e, kLog2e));
+        y.x = max_nan(y.x, kTiny), y.y = max_nan(y.y, kTiny);
+        const float2 e = make_float2(exp2_fast(y.x), exp2_fast(y.y));
+        s2 = add2(s2, e);
+        t2 = fma2(e, y, t2);
       }
     }
+  };
+  const uint32_t whole = (vocab + off) / kUnit;  // units before this one end inside the row; unit 0 may begin before it
+  for (uint32_t u = u0; u < u1; u += kThreads * kUnits) {
+    if (u > 0 && u + kThreads * kUnits <= min(u1, whole)) round(u, std::true_type());
+    else round(u, std::false_type());
   }
+  r.s = s2.x + s2.y, r.t = t2.x + t2.y;
   if (kTop) {
     __syncthreads();
     if (sh.lost) {
@@ -373,6 +412,7 @@ token_logprob_grad_kernel(LogprobGradArgs a, uint32_t per_row, unsigned int* __r
 }
 
 // ------------------------------------------------------------------ launchers
+constexpr int kWide = 256, kNarrow = 128;
 int launch_token_logprob(int dtype, const LogprobArgs& a, unsigned int* status, const LaunchShape& shape,
                          cudaStream_t stream) {
   // Rows are split over a cluster until there are about two CTAs for every SM, as long as a CTA keeps a round.
@@ -384,8 +424,8 @@ int launch_token_logprob(int dtype, const LogprobArgs& a, unsigned int* status, 
     using T = decltype(t);
     const dim3 grid(static_cast<unsigned>(a.rows * cluster));
     auto go = [&](auto kernel, unsigned threads) { launch_lm(kernel, grid, threads, 0, cluster, stream, shape.chained, a, cluster, status); };
-    if (narrow) a.k ? go(token_logprob_kernel<T, 128, true>, 128) : go(token_logprob_kernel<T, 128, false>, 128);
-    else a.k ? go(token_logprob_kernel<T, 512, true>, 512) : go(token_logprob_kernel<T, 512, false>, 512);
+    if (narrow) a.k ? go(token_logprob_kernel<T, kNarrow, true>, kNarrow) : go(token_logprob_kernel<T, kNarrow, false>, kNarrow);
+    else a.k ? go(token_logprob_kernel<T, kWide, true>, kWide) : go(token_logprob_kernel<T, kWide, false>, kWide);
   });
   return 1;
 }
