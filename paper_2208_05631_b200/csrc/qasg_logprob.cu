@@ -163,7 +163,7 @@ __device__ __noinline__ void push_round(RowShared& sh, const T* x, uint32_t k, u
 }
 
 template <typename T, int kThreads, bool kTop>
-__global__ void __launch_bounds__(kThreads, 1024 / kThreads)
+__global__ void __launch_bounds__(kThreads, 768 / kThreads)
 token_logprob_kernel(LogprobArgs a, uint32_t cluster, unsigned int* __restrict__ status) {
   constexpr int kUnits = kRoundUnits<T>;
   __shared__ RowShared sh;
@@ -201,16 +201,27 @@ token_logprob_kernel(LogprobArgs a, uint32_t cluster, unsigned int* __restrict__
   float base = 0.f;                         // m, 0 while m is -inf
   float bound = -INFINITY;
   uint32_t meet = u0;  // the next round at which the list is cut back: 0, 4, 16, 64, ...
-  // One round of units from u on; inside: every unit lies in this part and inside the row.
-  auto round = [&](uint32_t u, auto inside) {
-    constexpr bool kInside = decltype(inside)::value;
+  // Rounds of units: the next one's loads are under way while one is worked on.
+  const uint32_t whole = min(u1, (vocab + off) / kUnit);  // units before this one end inside the row; unit 0 may begin before it
+  auto is_inside = [&](uint32_t u) { return u > 0 && u + kThreads * kUnits <= whole; };
+  auto load = [&](uint32_t u, Unit<T>(&raw)[kUnits]) {
     const int64_t c0 = static_cast<int64_t>(u + tid) * kUnit - off;
-    Unit<T> raw[kUnits];
-    float top[kUnits];
+    if (is_inside(u)) {
 #pragma unroll
-    for (int j = 0; j < kUnits; ++j)
-      raw[j] = kInside ? load_unit(x + c0 + j * kThreads * kUnit)
-                       : load_row_unit<T>(x, c0 + j * kThreads * kUnit, u + j * kThreads + tid < u1 ? vocab : 0);
+      for (int j = 0; j < kUnits; ++j) raw[j] = load_unit(x + c0 + j * kThreads * kUnit);
+    } else {
+#pragma unroll
+      for (int j = 0; j < kUnits; ++j)
+        raw[j] = load_row_unit<T>(x, c0 + j * kThreads * kUnit, u + j * kThreads + tid < u1 ? vocab : 0);
+    }
+  };
+  Unit<T> raw[kUnits];
+  if (u0 < u1) load(u0, raw);
+  for (uint32_t u = u0; u < u1; u += kThreads * kUnits) {
+    Unit<T> next[kUnits];
+    if (u + kThreads * kUnits < u1) load(u + kThreads * kUnits, next);
+    const int64_t c0 = static_cast<int64_t>(u + tid) * kUnit - off;
+    float top[kUnits];
     float m = -INFINITY;
 #pragma unroll
     for (int j = 0; j < kUnits; ++j) {
@@ -254,7 +265,7 @@ token_logprob_kernel(LogprobArgs a, uint32_t cluster, unsigned int* __restrict__
             uint32_t bits = 0;
 #pragma unroll
             for (int k = 0; k < kUnit; ++k) bits |= v[k] < bound ? 0u : 1u << k;
-            if (!kInside) {  // not what lies outside the row, or in another part
+            if (!is_inside(u)) {  // not what lies outside the row, or in another part
               const int64_t c = c0 + j * kThreads * kUnit;
               if (c < 0) bits &= 0xffu << -c;
               if (c + kUnit > vocab) bits &= c >= vocab ? 0u : 0xffu >> (c + kUnit - vocab);
@@ -285,11 +296,8 @@ token_logprob_kernel(LogprobArgs a, uint32_t cluster, unsigned int* __restrict__
         t2 = fma2(e, y, t2);
       }
     }
-  };
-  const uint32_t whole = (vocab + off) / kUnit;  // units before this one end inside the row; unit 0 may begin before it
-  for (uint32_t u = u0; u < u1; u += kThreads * kUnits) {
-    if (u > 0 && u + kThreads * kUnits <= min(u1, whole)) round(u, std::true_type());
-    else round(u, std::false_type());
+#pragma unroll
+    for (int j = 0; j < kUnits; ++j) raw[j] = next[j];
   }
   r.s = s2.x + s2.y, r.t = t2.x + t2.y;
   if (kTop) {
