@@ -3,10 +3,10 @@
 //   dx_v = p_v (g_lse - g_logprob - g_entropy (log p_v + entropy)) + [v = token] g_logprob.
 // Forward: one pass over the logits.  A thread keeps the running maximum m, s = sum 2^y and t = sum y 2^y with
 // y = (x - m) log2(e); when m grows by d (in units of log2), s becomes 2^-d s and t becomes 2^-d (t - d s).
-// Alternatives: a candidate is an element at least as large as a lower bound of the k-th largest value; candidates
-// go to a list in shared memory.  The bound comes from the first round of loads (its exact k-th largest element,
-// found by cutting that round's candidates back to k), and again from rounds 4, 16, 64, ...; in between the warps
-// of a CTA do not meet.  A row with more candidates than the list holds (rising values, ties) is scanned again for them alone.
+// Alternatives: the smallest of the largest elements of g >= k groups of threads is at most the k-th largest
+// element, a bound that costs one meeting of the warps; it is taken after rounds 0, 1, 2, 4, 8, ... of loads, and
+// units that reach it are noted.  At the end the noted units' elements that reach the last bound are ranked.  A
+// row with more of either than there is room for (rising values, ties) is scanned again for them alone.
 // A row is shared by the CTAs of a cluster where there are fewer rows than the GPU has room for.
 #include <cooperative_groups.h>
 
@@ -18,7 +18,7 @@ namespace cg = cooperative_groups;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kTiny = -160.f;  // 2^kTiny is 0 in fp32: stands for every smaller power, so that 0 * y is 0
 template <typename T> constexpr int kRoundUnits = sizeof(T) == 4 ? 2 : 4;  // units a thread loads per round: 64 bytes
-constexpr int kListSize = 1024;  // candidates a CTA has room for
+constexpr int kListSize = 1024;  // units and elements a CTA has room to note
 constexpr int kMaxCluster = 8;
 
 // 2^y within 2 units in the last place; below 2^-126 it is 0.
@@ -87,6 +87,23 @@ template <> __device__ __forceinline__ float unit_top<float>(const Unit<float>& 
   return m;
 }
 
+// The value as a bf16 pair, rounded down (used for bf16 alone).
+__device__ __forceinline__ uint32_t pair_word(__nv_bfloat16, float v) {
+  const uint32_t b = __bfloat16_as_ushort(__float2bfloat16_rd(v));
+  return b | (b << 16);
+}
+template <typename T> __device__ __forceinline__ uint32_t pair_word(T, float) { return 0u; }
+// A unit with everything below the floor raised to it: two bf16 values in an instruction; other types as they are.
+__device__ __forceinline__ Unit<__nv_bfloat16> raised(Unit<__nv_bfloat16> u, uint32_t floor2) {
+#pragma unroll
+  for (int i = 0; i < kUnit / 2; ++i) {
+    const __nv_bfloat162 v = __hmax2_nan(*reinterpret_cast<const __nv_bfloat162*>(&u.w[i]), *reinterpret_cast<const __nv_bfloat162*>(&floor2));
+    u.w[i] = *reinterpret_cast<const uint32_t*>(&v);
+  }
+  return u;
+}
+template <typename T> __device__ __forceinline__ Unit<T> raised(const Unit<T>& u, uint32_t) { return u; }
+
 struct RowSums {
   float m, s, t;
 };
@@ -105,10 +122,11 @@ __device__ __forceinline__ RowSums join(RowSums a, RowSums o) {
 struct RowShared {
   unsigned long long list[kListSize];
   unsigned long long best[kMaxTop];
-  float group_max[32];
+  uint32_t units[kListSize];
+  float group_max[2][32];
   RowSums warp_sums[32];
   RowSums sums;
-  unsigned int count, lost;
+  unsigned int count, unit_count, lost;
   unsigned long long bound;
 };
 
@@ -191,16 +209,22 @@ token_logprob_kernel(LogprobArgs a, uint32_t cluster, unsigned int* __restrict__
       return;
     }
   }
-  if (kTop && tid == 0) sh.count = 0, sh.lost = 0, sh.bound = 0;
+  if (kTop && tid == 0) sh.count = 0, sh.unit_count = 0, sh.lost = 0, sh.bound = 0;
   // units on 16-byte boundaries: unit u holds columns 8u - off .. 8u - off + 7
   const uint32_t off = static_cast<uint32_t>((reinterpret_cast<uintptr_t>(x) & 15u) / sizeof(T));
   const uint32_t units = (vocab + off + kUnit - 1) / kUnit, per_part = (units + cluster - 1) / cluster;
   const uint32_t u0 = part * per_part, u1 = min(units, u0 + per_part);
   RowSums r = {-INFINITY, 0.f, 0.f};
-  float2 s2 = {0.f, 0.f}, t2 = {0.f, 0.f};  // s and t of the even and the odd columns
-  float base = 0.f;                         // m, 0 while m is -inf
+  // s and t of the even and the odd columns, with y = x log2(e) - ref, ref = m log2(e) rounded (0 while m is -inf).
+  // Where |m| > kHuge any two different values are further apart than fp32's exponents reach: y = (x - m) log2(e)
+  // there, which does not overflow.
+  constexpr float kHuge = 1e30f;
+  float2 s2 = {0.f, 0.f}, t2 = {0.f, 0.f};
+  float ref = 0.f;
+  bool huge = false;
+  uint32_t floor2 = pair_word(T(), -300.f);  // bf16: what is far below m, -inf among it, is raised to about m - 300
   float bound = -INFINITY;
-  uint32_t meet = u0;  // the next round at which the list is cut back: 0, 4, 16, 64, ...
+  uint32_t meet = u0, meetings = 0;  // the first unit of the next round after which the bound is taken
   // Rounds of units: the next one's loads are under way while one is worked on.
   const uint32_t whole = min(u1, (vocab + off) / kUnit);  // units before this one end inside the row; unit 0 may begin before it
   auto is_inside = [&](uint32_t u) { return u > 0 && u + kThreads * kUnits <= whole; };
@@ -215,11 +239,7 @@ token_logprob_kernel(LogprobArgs a, uint32_t cluster, unsigned int* __restrict__
         raw[j] = load_row_unit<T>(x, c0 + j * kThreads * kUnit, u + j * kThreads + tid < u1 ? vocab : 0);
     }
   };
-  Unit<T> raw[kUnits];
-  if (u0 < u1) load(u0, raw);
-  for (uint32_t u = u0; u < u1; u += kThreads * kUnits) {
-    Unit<T> next[kUnits];
-    if (u + kThreads * kUnits < u1) load(u + kThreads * kUnits, next);
+  auto work = [&](uint32_t u, const Unit<T>(&raw)[kUnits]) {
     const int64_t c0 = static_cast<int64_t>(u + tid) * kUnit - off;
     float top[kUnits];
     float m = -INFINITY;
@@ -229,83 +249,111 @@ token_logprob_kernel(LogprobArgs a, uint32_t cluster, unsigned int* __restrict__
       m = max_nan(m, top[j]);
     }
     if (!(m <= r.m)) {
-      const float d = max_nan((r.m - m) * kLog2e, kTiny), c = exp2_fast(d);
+      const bool apart = huge || r.m == -INFINITY;
+      const float old = ref;
+      huge = fabsf(m) > kHuge;
+      ref = huge ? 0.f : m * kLog2e;
+      const float d = huge || apart ? kTiny : max_nan(old - ref, kTiny), c = exp2_fast(d);
       t2 = mul2(make_float2(c, c), fma2(s2, make_float2(d, d), t2));
       s2 = mul2(make_float2(c, c), s2);
       r.m = m;
-      base = m;
+      floor2 = pair_word(T(), m - 300.f);
     }
     if (kTop) {
-      if (u == u0) {
-        // The smallest of the largest elements of g groups is at most the g-th largest element of all, so with
-        // g >= k at most the k-th: g groups of threads, g the power of two from k on (up to 32).
+      if (u == meet) {
         constexpr int kLanes = kThreads / 32;
-        float g = m == m ? m : INFINITY;
+        float g = r.m == r.m ? r.m : INFINITY;
 #pragma unroll
         for (int s = kLanes / 2; s > 0; s >>= 1) g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, s));
-        if (tid % kLanes == 0) sh.group_max[tid / kLanes] = g;
+        if (tid % kLanes == 0) sh.group_max[meetings & 1u][tid / kLanes] = g;
         __syncthreads();
-        g = sh.group_max[tid & 31];
-        const uint32_t wide = 32u >> (32 - __clz(a.k - 1));  // of the 32 groups of kLanes threads in one of the g
+        g = sh.group_max[meetings & 1u][tid & 31];
+        const uint32_t wide = 32u >> (32 - __clz(a.k - 1));  // g = the power of two from k on: so many of the 32 in one
         for (uint32_t s = 1; s < 32; s <<= 1) {
           const float o = __shfl_xor_sync(0xffffffffu, g, s);
           g = s < wide ? fmaxf(g, o) : fminf(g, o);
         }
-        if (tid == 0) sh.bound = static_cast<unsigned long long>(value_order(g)) << 32;
         bound = g;
-        __syncthreads();
+        ++meetings;
+        meet = u0 + max(2u * (u - u0), static_cast<uint32_t>(kThreads * kUnits));
       }
-      uint32_t pending = 0;
       if (!(m < bound)) {
 #pragma unroll
         for (int j = 0; j < kUnits; ++j)
           if (!(top[j] < bound)) {
-            float v[kUnit];
-            unit_floats(raw[j], v);
-            uint32_t bits = 0;
-#pragma unroll
-            for (int k = 0; k < kUnit; ++k) bits |= v[k] < bound ? 0u : 1u << k;
-            if (!is_inside(u)) {  // not what lies outside the row, or in another part
-              const int64_t c = c0 + j * kThreads * kUnit;
-              if (c < 0) bits &= 0xffu << -c;
-              if (c + kUnit > vocab) bits &= c >= vocab ? 0u : 0xffu >> (c + kUnit - vocab);
-              if (u + j * kThreads + tid >= u1) bits = 0u;
-            }
-            pending |= bits << (j * kUnit);
+            const uint32_t w = u + j * kThreads + tid, at = atomicAdd(&sh.unit_count, 1u);
+            if (at < kListSize) sh.units[at] = w;
           }
       }
-      if (u == meet) {
-        push_round<T, kThreads>(sh, x, a.k, pending, c0);
-        meet = u0 + max(4u * (u - u0), 4u * kThreads * kUnits);
-        bound = key_value(sh.bound);
-        if (bound != bound) bound = INFINITY;  // k NaNs: nothing but another NaN passes
-      } else if (pending) {
-        if (push_pending<T, kThreads>(sh, x, pending, c0)) sh.lost = 1u;
+    }
+    if (!huge) {
+#pragma unroll
+      for (int j = 0; j < kUnits; ++j) {
+        float v[kUnit];
+        unit_floats(raised(raw[j], floor2), v);
+#pragma unroll
+        for (int k = 0; k < kUnit; k += 2) {
+          float2 y = fma2(make_float2(v[k], v[k + 1]), make_float2(kLog2e, kLog2e), make_float2(-ref, -ref));
+          if (!std::is_same<T, __nv_bfloat16>::value) y.x = max_nan(y.x, kTiny), y.y = max_nan(y.y, kTiny);
+          const float2 e = make_float2(exp2_fast(y.x), exp2_fast(y.y));
+          s2 = add2(s2, e);
+          t2 = fma2(e, y, t2);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < kUnits; ++j) {
+        float v[kUnit];
+        unit_floats(raw[j], v);
+#pragma unroll
+        for (int k = 0; k < kUnit; ++k) {
+          const float y = max_nan((v[k] - r.m) * kLog2e, kTiny), e = exp2_fast(y);
+          s2.x += e;
+          t2.x = fmaf(e, y, t2.x);
+        }
       }
     }
-#pragma unroll
-    for (int j = 0; j < kUnits; ++j) {
-      float v[kUnit];
-      unit_floats(raw[j], v);
-#pragma unroll
-      for (int k = 0; k < kUnit; k += 2) {
-        float2 y = mul2(add2(make_float2(v[k], v[k + 1]), make_float2(-base, -base)), make_float2(kLog2e, kLog2e));
-        y.x = max_nan(y.x, kTiny), y.y = max_nan(y.y, kTiny);
-        const float2 e = make_float2(exp2_fast(y.x), exp2_fast(y.y));
-        s2 = add2(s2, e);
-        t2 = fma2(e, y, t2);
-      }
+  };
+  if (u0 < u1) {
+    Unit<T> first[kUnits], second[kUnits];
+    constexpr uint32_t kStep = kThreads * kUnits;
+    load(u0, first);
+    for (uint32_t u = u0;;) {
+      if (u + kStep < u1) load(u + kStep, second);
+      work(u, first);
+      if ((u += kStep) >= u1) break;
+      if (u + kStep < u1) load(u + kStep, first);
+      work(u, second);
+      if ((u += kStep) >= u1) break;
     }
-#pragma unroll
-    for (int j = 0; j < kUnits; ++j) raw[j] = next[j];
   }
   r.s = s2.x + s2.y, r.t = t2.x + t2.y;
+  if (!huge && r.m > -INFINITY) {  // from ref to m log2(e) itself: they differ by a rounding
+    const float d = -fmaf(r.m, kLog2e, -ref), c = exp2_fast(d);
+    r.t = c * fmaf(d, r.s, r.t);
+    r.s *= c;
+  }
   if (kTop) {
+    if (tid == 0) sh.bound = static_cast<unsigned long long>(value_order(bound)) << 32;
     __syncthreads();
-    if (sh.lost) {
-      // the k-th best of what was kept is a far better bound: once more, from the start, meeting at every round
-      cut_list<kThreads>(sh, a.k);
-      if (tid == 0) sh.count = 0, sh.bound = sh.best[a.k - 1];
+    bool again = sh.unit_count > kListSize;
+    if (!again) {
+      for (uint32_t i = tid; i < sh.unit_count; i += kThreads) {
+        const uint32_t w = sh.units[i];
+        const int64_t c0 = static_cast<int64_t>(w) * kUnit - off;
+        float v[kUnit];
+        unit_floats(load_row_unit<T>(x, c0, vocab), v);
+        uint32_t bits = 0;
+#pragma unroll
+        for (int k = 0; k < kUnit; ++k) bits |= v[k] < bound || w >= u1 || c0 + k < 0 || c0 + k >= vocab ? 0u : 1u << k;
+        if (push_pending<T, kThreads>(sh, x, bits, c0)) sh.lost = 1u;
+      }
+      __syncthreads();
+      again = sh.lost;
+    }
+    if (again) {  // too many: once more from the start, cutting the list back to its k best at every round
+      __syncthreads();
+      if (tid == 0) sh.count = 0;
       __syncthreads();
       for (uint32_t u = u0; u < u1; u += kThreads * kUnits) {
         const int64_t c0 = static_cast<int64_t>(u + tid) * kUnit - off;
