@@ -3,10 +3,10 @@
 //   dx_v = p_v (g_lse - g_logprob - g_entropy (log p_v + entropy)) + [v = token] g_logprob.
 // Forward: one pass over the logits.  A thread keeps the running maximum m, s = sum 2^y and t = sum y 2^y with
 // y = (x - m) log2(e); when m grows by d (in units of log2), s becomes 2^-d s and t becomes 2^-d (t - d s).
-// Alternatives: the smallest of the largest elements of g >= k groups of threads is at most the k-th largest
-// element, a bound that costs one meeting of the warps; it is taken after rounds 0, 1, 2, 4, 8, ... of loads, and
-// units that reach it are noted.  At the end the noted units' elements that reach the last bound are ranked.  A
-// row with more of either than there is room for (rising values, ties) is scanned again for them alone.
+// Alternatives: the k-th largest of the maxima of 64 groups of threads is at most the k-th largest element.  This
+// bound is taken after rounds 0, 2, 8, 32, ... of loads (one meeting of the warps each), and units that reach it are
+// noted.  At the end the noted units' elements that reach the last bound are ranked.  A row with more of either
+// than there is room for (rising values, ties) is scanned again for them alone.
 // A row is shared by the CTAs of a cluster where there are fewer rows than the GPU has room for.
 #include <cooperative_groups.h>
 
@@ -20,6 +20,7 @@ constexpr float kTiny = -160.f;  // 2^kTiny is 0 in fp32: stands for every small
 template <typename T> constexpr int kRoundUnits = sizeof(T) == 4 ? 2 : 4;  // units a thread loads per round: 64 bytes
 constexpr int kListSize = 1024;  // units and elements a CTA has room to note
 constexpr int kMaxCluster = 8;
+constexpr int kGroups = 64;      // of threads; more than kMaxTop, so that few elements reach the k-th largest maximum
 
 // 2^y within 2 units in the last place; below 2^-126 it is 0.
 __device__ __forceinline__ float exp2_fast(float y) {
@@ -123,17 +124,31 @@ struct RowShared {
   unsigned long long list[kListSize];
   unsigned long long best[kMaxTop];
   uint32_t units[kListSize];
-  float group_max[2][32];
+  uint32_t maxima[2][kGroups];  // in value_order
   RowSums warp_sums[32];
   RowSums sums;
-  unsigned int count, unit_count, lost;
+  unsigned int count, unit_count, lost, kept;
   unsigned long long bound;
 };
 
-// Cuts the list back to its k best, in order, also in `best`; raises the bound.  Called by all threads; what
-// they pushed before is seen.  Keys are distinct, so an element's rank is the number of larger ones.
+// A value that at least k of the groups' maxima reach, within 2^-7 of the largest such: their upper 16 bits are
+// searched bit by bit.  Every warp finds it for itself.
+__device__ __forceinline__ float kth_largest(const uint32_t* maxima, uint32_t k) {
+  const uint32_t v0 = maxima[threadIdx.x & 31], v1 = maxima[(threadIdx.x & 31) + 32];
+  uint32_t t = 0;
+#pragma unroll
+  for (uint32_t bit = 1u << 31; bit >= 1u << 16; bit >>= 1) {
+    const uint32_t next = t | bit;
+    if (__popc(__ballot_sync(0xffffffffu, v0 >= next)) + __popc(__ballot_sync(0xffffffffu, v1 >= next)) >= k) t = next;
+  }
+  if (t < 0x00800000u) return -INFINITY;
+  return t > 0xff800000u ? INFINITY : key_value(static_cast<unsigned long long>(t) << 32);
+}
+
+// Ranks the list's elements; the k best, in order, go to `best`.  Called by all threads; what they pushed before is
+// seen, and so are the results after it.  Keys are distinct, so an element's rank is the number of larger ones.
 template <int kThreads>
-__device__ __forceinline__ void cut_list(RowShared& sh, uint32_t k) {
+__device__ __forceinline__ uint32_t rank_list(RowShared& sh, uint32_t k) {
   __syncthreads();
   const uint32_t n = min(sh.count, static_cast<unsigned>(kListSize));
   for (uint32_t i = threadIdx.x; i < n; i += kThreads) {
@@ -143,7 +158,13 @@ __device__ __forceinline__ void cut_list(RowShared& sh, uint32_t k) {
     if (rank < k) sh.best[rank] = key;
   }
   __syncthreads();
-  const uint32_t kept = min(n, k);
+  return min(n, k);
+}
+
+// Cuts the list back to its k best and raises the bound.
+template <int kThreads>
+__device__ __forceinline__ void cut_list(RowShared& sh, uint32_t k) {
+  const uint32_t kept = rank_list<kThreads>(sh, k);
   for (uint32_t i = threadIdx.x; i < kept; i += kThreads) sh.list[i] = sh.best[i];
   if (threadIdx.x == 0) {
     sh.count = kept;
@@ -261,21 +282,15 @@ token_logprob_kernel(LogprobArgs a, uint32_t cluster, unsigned int* __restrict__
     }
     if (kTop) {
       if (u == meet) {
-        constexpr int kLanes = kThreads / 32;
-        float g = r.m == r.m ? r.m : INFINITY;
+        uint32_t* maxima = sh.maxima[meetings & 1u];
+        uint32_t largest = value_order(r.m);
 #pragma unroll
-        for (int s = kLanes / 2; s > 0; s >>= 1) g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, s));
-        if (tid % kLanes == 0) sh.group_max[meetings & 1u][tid / kLanes] = g;
+        for (int s = kThreads / kGroups / 2; s > 0; s >>= 1) largest = max(largest, __shfl_xor_sync(0xffffffffu, largest, s));
+        if (tid % (kThreads / kGroups) == 0) maxima[tid / (kThreads / kGroups)] = largest;
         __syncthreads();
-        g = sh.group_max[meetings & 1u][tid & 31];
-        const uint32_t wide = 32u >> (32 - __clz(a.k - 1));  // g = the power of two from k on: so many of the 32 in one
-        for (uint32_t s = 1; s < 32; s <<= 1) {
-          const float o = __shfl_xor_sync(0xffffffffu, g, s);
-          g = s < wide ? fmaxf(g, o) : fminf(g, o);
-        }
-        bound = g;
+        bound = kth_largest(maxima, a.k);
         ++meetings;
-        meet = u0 + max(2u * (u - u0), static_cast<uint32_t>(kThreads * kUnits));
+        meet = u0 + max(4u * (u - u0), 2u * kThreads * kUnits);
       }
       if (!(m < bound)) {
 #pragma unroll
@@ -385,28 +400,30 @@ token_logprob_kernel(LogprobArgs a, uint32_t cluster, unsigned int* __restrict__
     r = join(r, o);
   }
   if ((tid & 31) == 0) sh.warp_sums[tid >> 5] = r;
-  if (kTop) cut_list<kThreads>(sh, a.k);
-  else __syncthreads();
+  if (kTop) {
+    const uint32_t kept = rank_list<kThreads>(sh, a.k);
+    if (tid == 0) sh.kept = kept;
+  } else {
+    __syncthreads();
+  }
   r = sh.warp_sums[0];
 #pragma unroll
   for (int i = 1; i < kThreads / 32; ++i) r = join(r, sh.warp_sums[i]);
   if (cluster > 1) {
     cg::cluster_group group = cg::this_cluster();
     if (tid == 0) sh.sums = r;
+    if (kTop && tid == 0) sh.count = 0;
     group.sync();
     if (part == 0) {
-      for (uint32_t o = 1; o < cluster; ++o) {
+      for (uint32_t o = 0; o < cluster; ++o) {
         const RowShared* other = group.map_shared_rank(&sh, o);
-        r = join(r, other->sums);
-        if (kTop && tid < other->count) {
-          const uint32_t at = atomicAdd(&sh.count, 1u);
-          sh.list[at] = other->list[tid];
-        }
+        if (o) r = join(r, other->sums);
+        if (kTop && tid < other->kept) sh.list[atomicAdd(&sh.count, 1u)] = other->best[tid];
       }
     }
     group.sync();  // the other CTAs' shared memory has been read
     if (part) return;
-    if (kTop) cut_list<kThreads>(sh, a.k);
+    if (kTop) rank_list<kThreads>(sh, a.k);
   }
   const float log_s = logf(r.s);
   const bool empty = r.m == -INFINITY;  // every logit is -inf
@@ -468,20 +485,21 @@ token_logprob_grad_kernel(LogprobGradArgs a, uint32_t per_row, unsigned int* __r
 }
 
 // ------------------------------------------------------------------ launchers
-constexpr int kWide = 256, kNarrow = 128;
+constexpr int kManyRows = 128, kFewRows = 512;  // threads of a CTA
 int launch_token_logprob(int dtype, const LogprobArgs& a, unsigned int* status, const LaunchShape& shape,
                          cudaStream_t stream) {
-  // Rows are split over a cluster until there are about two CTAs for every SM, as long as a CTA keeps a round.
-  const bool narrow = a.vocab <= 4096;
+  // With at least a row for every SM a row is one CTA's, small ones, of which six stand on an SM: their meetings
+  // cost least.  Fewer rows are split over clusters of large CTAs as long as a CTA keeps a round of loads.
+  const bool many = a.rows >= static_cast<uint64_t>(shape.sm_count) || a.vocab <= kManyRows * 32;
   uint32_t cluster = 1;
-  if (!narrow)
-    while (cluster < kMaxCluster && a.rows * cluster < static_cast<uint64_t>(shape.sm_count) && a.vocab / cluster > 16384) cluster *= 2;
+  if (!many)
+    while (cluster < kMaxCluster && a.rows * cluster < static_cast<uint64_t>(shape.sm_count) && a.vocab / cluster > kFewRows * 32) cluster *= 2;
   with_dtype(dtype, [&](auto t) {
     using T = decltype(t);
     const dim3 grid(static_cast<unsigned>(a.rows * cluster));
     auto go = [&](auto kernel, unsigned threads) { launch_lm(kernel, grid, threads, 0, cluster, stream, shape.chained, a, cluster, status); };
-    if (narrow) a.k ? go(token_logprob_kernel<T, kNarrow, true>, kNarrow) : go(token_logprob_kernel<T, kNarrow, false>, kNarrow);
-    else a.k ? go(token_logprob_kernel<T, kWide, true>, kWide) : go(token_logprob_kernel<T, kWide, false>, kWide);
+    if (many) a.k ? go(token_logprob_kernel<T, kManyRows, true>, kManyRows) : go(token_logprob_kernel<T, kManyRows, false>, kManyRows);
+    else a.k ? go(token_logprob_kernel<T, kFewRows, true>, kFewRows) : go(token_logprob_kernel<T, kFewRows, false>, kFewRows);
   });
   return 1;
 }
