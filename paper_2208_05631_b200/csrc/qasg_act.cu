@@ -26,7 +26,7 @@ __device__ __forceinline__ ActItem act_item(uint64_t item, uint32_t per_row) {
   return a;
 }
 
-template <typename T>
+template <typename T, bool kAligned>
 __global__ void __launch_bounds__(kActWarps * 32)
 act_pack_kernel(const T* __restrict__ x, uint64_t ld_x, ActView act, uint64_t items, uint32_t per_row,
                 unsigned int* __restrict__ status) {
@@ -41,7 +41,7 @@ act_pack_kernel(const T* __restrict__ x, uint64_t ld_x, ActView act, uint64_t it
   float v[kActItemUnits][kUnit];
 #pragma unroll
   for (int j = 0; j < kActItemUnits; ++j)
-    load_values<T>(row, a.col + (j * 32 + lane) * kUnit, act.cols, 0.f, v[j]);
+    load_values<T, kAligned>(row, a.col + (j * 32 + lane) * kUnit, act.cols, 0.f, v[j]);
   bool bad = false;
 #pragma unroll
   for (int j = 0; j < kActItemUnits; ++j) {
@@ -57,7 +57,7 @@ act_pack_kernel(const T* __restrict__ x, uint64_t ld_x, ActView act, uint64_t it
   if (bad) atomicOr(status, kFlagNonFinite);
 }
 
-template <typename T>
+template <typename T, bool kAligned>
 __global__ void __launch_bounds__(kActWarps * 32)
 act_unpack_kernel(ActView act, T* __restrict__ x, uint64_t ld_x, uint64_t items, uint32_t per_row) {
   const uint64_t item = static_cast<uint64_t>(blockIdx.x) * kActWarps + (threadIdx.x >> 5);
@@ -71,6 +71,7 @@ act_unpack_kernel(ActView act, T* __restrict__ x, uint64_t ld_x, uint64_t items,
 #pragma unroll
   for (int j = 0; j < kActItemUnits; ++j) {
     const uint32_t c = a.col + (j * 32 + lane) * kUnit;
+    codes[j] = make_uint2(0u, 0u), exps[j] = 7u;
     if (c >= act.cols) continue;
     codes[j] = __ldcs(reinterpret_cast<const uint2*>(act.codes + a.row * act.ld_codes + c));
     exps[j] = act.exps[a.row * act.ld_exps + c / kActBlock];
@@ -78,13 +79,12 @@ act_unpack_kernel(ActView act, T* __restrict__ x, uint64_t ld_x, uint64_t items,
 #pragma unroll
   for (int j = 0; j < kActItemUnits; ++j) {
     const uint32_t c = a.col + (j * 32 + lane) * kUnit;
-    if (c >= act.cols) continue;
     float v[kUnit];
     code_floats(codes[j], v);
     const float unit = act_unit(exps[j]);
 #pragma unroll
     for (int k = 0; k < kUnit; ++k) v[k] *= unit;
-    store_values<T>(x + a.row * ld_x, c, act.cols, v);
+    store_row_unit<T, kAligned>(x + a.row * ld_x, c, act.cols, v);
   }
 }
 
@@ -93,9 +93,9 @@ int launch_act_pack(int dtype, const void* x, uint64_t ld_x, const ActView& act,
   const uint32_t per_row = (act.cols + kActItem - 1) / kActItem;
   const uint64_t items = act.rows * per_row;
   const dim3 grid(static_cast<unsigned>((items + kActWarps - 1) / kActWarps));
-  with_dtype(dtype, [&](auto t) {
+  with_dtype_aligned(dtype, rows_aligned(dtype, x, ld_x), [&](auto t, auto aligned) {
     using T = decltype(t);
-    launch_lm(act_pack_kernel<T>, grid, kActWarps * 32, 0, 1, stream, shape.chained, static_cast<const T*>(x), ld_x, act,
+    launch_lm(act_pack_kernel<T, decltype(aligned)::value>, grid, kActWarps * 32, 0, 1, stream, shape.chained, static_cast<const T*>(x), ld_x, act,
               items, per_row, status);
   });
   return 1;
@@ -106,9 +106,9 @@ int launch_act_unpack(const ActView& act, int dtype, void* x, uint64_t ld_x, con
   const uint32_t per_row = (act.cols + kActItem - 1) / kActItem;
   const uint64_t items = act.rows * per_row;
   const dim3 grid(static_cast<unsigned>((items + kActWarps - 1) / kActWarps));
-  with_dtype(dtype, [&](auto t) {
+  with_dtype_aligned(dtype, rows_aligned(dtype, x, ld_x), [&](auto t, auto aligned) {
     using T = decltype(t);
-    launch_lm(act_unpack_kernel<T>, grid, kActWarps * 32, 0, 1, stream, shape.chained, act, static_cast<T*>(x), ld_x, items,
+    launch_lm(act_unpack_kernel<T, decltype(aligned)::value>, grid, kActWarps * 32, 0, 1, stream, shape.chained, act, static_cast<T*>(x), ld_x, items,
               per_row);
   });
   return 1;

@@ -4,6 +4,8 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <type_traits>
+
 #include "qasg_device.cuh"
 
 namespace qasg {
@@ -74,34 +76,98 @@ template <typename T> __device__ __forceinline__ void set_value(Unit<T>& u, int 
 }
 template <> __device__ __forceinline__ void set_value<float>(Unit<float>& u, int k, float v) { u.w[k] = __float_as_uint(v); }
 
-// Values [i, i + 8) of a row of n values, `fill` outside the row; any alignment of the row.
-template <typename T>
-__device__ __forceinline__ void load_values(const T* row, int64_t i, int64_t n, float fill, float (&v)[kUnit]) {
-  if (i >= 0 && i + kUnit <= n && is_aligned16(row + i)) {
-    unit_floats(load_unit(row + i), v);
-  } else {
+// 4 words (kWords) from byte `shift` (below 16) on of the words x and what follows them.
+template <int kWords>
+__device__ __forceinline__ void shifted_words(const uint32_t (&x)[kWords + 4], uint32_t shift, uint32_t (&out)[kWords]) {
+  uint32_t y[kWords + 2], z[kWords + 1];
 #pragma unroll
-    for (int k = 0; k < kUnit; ++k) v[k] = (i + k >= 0 && i + k < n) ? to_float(row[i + k]) : fill;
-  }
+  for (int i = 0; i < kWords + 2; ++i) y[i] = shift & 8u ? x[i + 2] : x[i];
+#pragma unroll
+  for (int i = 0; i < kWords + 1; ++i) z[i] = shift & 4u ? y[i + 1] : y[i];
+#pragma unroll
+  for (int i = 0; i < kWords; ++i) out[i] = __funnelshift_r(z[i], z[i + 1], (shift & 2u) * 8);
 }
 
-template <typename T> __device__ __forceinline__ void store_unit(T* p, const float (&v)[kUnit]) {
-  uint4 q;
-  q.x = pack2(v[0], v[1], T()), q.y = pack2(v[2], v[3], T()), q.z = pack2(v[4], v[5], T()), q.w = pack2(v[6], v[7], T());
-  *reinterpret_cast<uint4*>(p) = q;
-}
-template <> __device__ __forceinline__ void store_unit<float>(float* p, const float (&v)[kUnit]) {
-  reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-  reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
-}
-template <typename T>
-__device__ __forceinline__ void store_values(T* row, int64_t i, int64_t n, const float (&v)[kUnit]) {
-  if (i >= 0 && i + kUnit <= n && is_aligned16(row + i)) {
-    store_unit(row + i, v);
+// The unit at column c of a row of n values, `fill` past its end.  kAligned: every row begins on a 16-byte boundary.
+// Otherwise the aligned words around a unit are read and shifted, as long as those lie in the row too.
+template <typename T, bool kAligned>
+__device__ __forceinline__ Unit<T> load_row_unit(const T* row, uint32_t c, uint32_t n, float fill) {
+  constexpr uint32_t kWords = sizeof(Unit<T>) / 4;
+  const uint32_t shift = kAligned ? 0u : static_cast<uint32_t>(reinterpret_cast<uintptr_t>(row)) & 15u;
+  Unit<T> u;
+  if (shift == 0 && c + kUnit <= n) {
+    u = load_unit(row + c);
+  } else if (!kAligned && shift && c >= shift / sizeof(T) && c + kUnit + (16u - shift) / sizeof(T) <= n) {
+    const uint4* q = reinterpret_cast<const uint4*>(row + c - shift / sizeof(T));
+    uint32_t x[kWords + 4];
+#pragma unroll
+    for (uint32_t k = 0; k < kWords / 4 + 1; ++k) {
+      const uint4 v = q[k];
+      x[4 * k] = v.x, x[4 * k + 1] = v.y, x[4 * k + 2] = v.z, x[4 * k + 3] = v.w;
+    }
+    shifted_words<kWords>(x, shift, u.w);
   } else {
 #pragma unroll
-    for (int k = 0; k < kUnit; ++k)
-      if (i + k >= 0 && i + k < n) row[i + k] = from_float<T>(v[k]);
+    for (int k = 0; k < kUnit; ++k) set_value(u, k, c + k < n ? to_float(row[c + k]) : fill);
+  }
+  return u;
+}
+template <typename T, bool kAligned>
+__device__ __forceinline__ void load_values(const T* row, uint32_t c, uint32_t n, float fill, float (&v)[kUnit]) {
+  unit_floats(load_row_unit<T, kAligned>(row, c, n, fill), v);
+}
+
+template <typename T> __device__ __forceinline__ Unit<T> pack_unit(const float (&v)[kUnit]) {
+  Unit<T> u;
+#pragma unroll
+  for (int i = 0; i < kUnit / 2; ++i) u.w[i] = pack2(v[2 * i], v[2 * i + 1], T());
+  return u;
+}
+template <> __device__ __forceinline__ Unit<float> pack_unit<float>(const float (&v)[kUnit]) {
+  Unit<float> u;
+#pragma unroll
+  for (int i = 0; i < kUnit; ++i) u.w[i] = __float_as_uint(v[i]);
+  return u;
+}
+template <typename T> __device__ __forceinline__ void store_unit(T* p, const Unit<T>& u) {
+#pragma unroll
+  for (int i = 0; i < static_cast<int>(sizeof(u) / 16); ++i)
+    reinterpret_cast<uint4*>(p)[i] = make_uint4(u.w[4 * i], u.w[4 * i + 1], u.w[4 * i + 2], u.w[4 * i + 3]);
+}
+// Stores values as the unit at column c of a row of n values.  Called by whole warps, the lanes' units one after the
+// other in the row; a lane with c >= n stores nothing.  Off a 16-byte boundary a lane stores the 16-byte words that its
+// unit begins in, with the last values of the unit before it; the first lane's first and the last lane's last values go
+// one by one.
+template <typename T, bool kAligned>
+__device__ __forceinline__ void store_row_unit(T* row, uint32_t c, uint32_t n, const float (&v)[kUnit]) {
+  constexpr int kWords = sizeof(Unit<T>) / 4;
+  const uint32_t shift = kAligned ? 0u : static_cast<uint32_t>(reinterpret_cast<uintptr_t>(row)) & 15u;
+  const Unit<T> u = pack_unit<T>(v);
+  uint32_t first = 0, end = kUnit;  // values that go one by one
+  if (shift == 0) {
+    if (c + kUnit <= n) {
+      store_unit(row + c, u);
+      return;
+    }
+  } else {
+    uint32_t x[kWords + 4];
+    Unit<T> w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = __shfl_up_sync(0xffffffffu, u.w[kWords - 4 + i], 1);
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) x[4 + i] = u.w[i];
+    shifted_words<kWords>(x, 16u - shift, w.w);
+    const uint32_t lane = threadIdx.x & 31, mine = kUnit - shift / sizeof(T);  // values in the words the unit begins in
+    if (lane > 0 && c + mine <= n) {
+      store_unit(row + c - shift / sizeof(T), w);
+      first = mine;
+    }
+    if (lane < 31 && c + kUnit + mine <= n) end = mine;  // the next lane stores the rest
+  }
+  if (first < end && c < n) {
+#pragma unroll
+    for (uint32_t k = 0; k < kUnit; ++k)
+      if (k >= first && k < end && c + k < n) row[c + k] = from_float<T>(v[k]);
   }
 }
 
@@ -171,6 +237,18 @@ template <typename F> inline void with_dtype(int dtype, F f) {
   if (dtype == kDtypeBf16) f(__nv_bfloat16());
   else if (dtype == kDtypeF16) f(__half());
   else f(0.f);
+}
+
+// Whether every row of a tensor begins on a 16-byte boundary.
+inline bool rows_aligned(int dtype, const void* p, uint64_t ld) {
+  return ((reinterpret_cast<uintptr_t>(p) | (ld * (dtype == kDtypeF32 ? 4 : 2))) & 15u) == 0;
+}
+// Calls f with a value of the element type and with std::true_type or std::false_type.
+template <typename F> inline void with_dtype_aligned(int dtype, bool aligned, F f) {
+  with_dtype(dtype, [&](auto t) {
+    if (aligned) f(t, std::true_type());
+    else f(t, std::false_type());
+  });
 }
 
 template <typename... KArgs, typename... Args>

@@ -64,7 +64,7 @@ __device__ __forceinline__ float key_value(unsigned long long key) {
 }
 
 // A unit of row values [i, i + 8) of n, -inf outside the row.
-template <typename T> __device__ __forceinline__ Unit<T> load_row_unit(const T* row, int64_t i, int64_t n) {
+template <typename T> __device__ __forceinline__ Unit<T> load_ragged_unit(const T* row, int64_t i, int64_t n) {
   if (i >= 0 && i + kUnit <= n) return load_unit(row + i);  // the caller's units lie on 16-byte boundaries
   Unit<T> u;
 #pragma unroll
@@ -257,11 +257,10 @@ token_logprob_kernel(LogprobArgs a, uint32_t cluster, unsigned int* __restrict__
     } else {
 #pragma unroll
       for (int j = 0; j < kUnits; ++j)
-        raw[j] = load_row_unit<T>(x, c0 + j * kThreads * kUnit, u + j * kThreads + tid < u1 ? vocab : 0);
+        raw[j] = load_ragged_unit<T>(x, c0 + j * kThreads * kUnit, u + j * kThreads + tid < u1 ? vocab : 0);
     }
   };
   auto work = [&](uint32_t u, const Unit<T>(&raw)[kUnits]) {
-    const int64_t c0 = static_cast<int64_t>(u + tid) * kUnit - off;
     float top[kUnits];
     float m = -INFINITY;
 #pragma unroll
@@ -357,7 +356,7 @@ token_logprob_kernel(LogprobArgs a, uint32_t cluster, unsigned int* __restrict__
         const uint32_t w = sh.units[i];
         const int64_t c0 = static_cast<int64_t>(w) * kUnit - off;
         float v[kUnit];
-        unit_floats(load_row_unit<T>(x, c0, vocab), v);
+        unit_floats(load_ragged_unit<T>(x, c0, vocab), v);
         uint32_t bits = 0;
 #pragma unroll
         for (int k = 0; k < kUnit; ++k) bits |= v[k] < bound || w >= u1 || c0 + k < 0 || c0 + k >= vocab ? 0u : 1u << k;
@@ -378,7 +377,7 @@ token_logprob_kernel(LogprobArgs a, uint32_t cluster, unsigned int* __restrict__
         for (int j = 0; j < kUnits; ++j) {
           const uint32_t w = u + j * kThreads + tid;
           float v[kUnit];
-          unit_floats(load_row_unit<T>(x, static_cast<int64_t>(w) * kUnit - off, w < u1 ? vocab : 0), v);
+          unit_floats(load_ragged_unit<T>(x, static_cast<int64_t>(w) * kUnit - off, w < u1 ? vocab : 0), v);
 #pragma unroll
           for (int k = 0; k < kUnit; ++k) {
             const int64_t c = static_cast<int64_t>(w) * kUnit - off + k;
@@ -442,7 +441,7 @@ token_logprob_kernel(LogprobArgs a, uint32_t cluster, unsigned int* __restrict__
 
 // ------------------------------------------------------------------ gradient
 constexpr int kGradThreads = 256, kGradUnits = 4;
-template <typename T>
+template <typename T, bool kAligned>
 __global__ void __launch_bounds__(kGradThreads)
 token_logprob_grad_kernel(LogprobGradArgs a, uint32_t per_row, unsigned int* __restrict__ status) {
   const uint64_t row = blockIdx.x / per_row;
@@ -457,30 +456,36 @@ token_logprob_grad_kernel(LogprobGradArgs a, uint32_t per_row, unsigned int* __r
   const float lse = a.lse[row], g_lp = a.g_logprob && a.tokens ? a.g_logprob[row] : 0.f;
   const float g_h = a.g_entropy ? a.g_entropy[row] : 0.f, g_lse = a.g_lse ? a.g_lse[row] : 0.f;
   const bool zero = skip || lse == -INFINITY;  // a padding row, or one whose logits are all -inf
-  // p (c0 - c1 y) with y = log2 p
-  const float c0 = g_lse - g_lp - (a.g_entropy ? g_h * a.entropy[row] : 0.f), c1 = g_h * kLn2;
-  const uint32_t off = static_cast<uint32_t>((reinterpret_cast<uintptr_t>(dx) & 15u) / sizeof(T));
-  const uint32_t u0 = part * (kGradThreads * kGradUnits) + threadIdx.x;
-  float v[kGradUnits][kUnit];
+  // p (c0s - c1 y) with y = log2 p
+  const float c0s = g_lse - g_lp - (a.g_entropy ? g_h * a.entropy[row] : 0.f), c1 = g_h * kLn2;
+  const uint32_t c0 = (part * (kGradThreads * kGradUnits) + threadIdx.x) * kUnit;
+  Unit<T> raw[kGradUnits];
   if (!zero) {
 #pragma unroll
-    for (int j = 0; j < kGradUnits; ++j)
-      load_values<T>(x, static_cast<int64_t>(u0 + j * kGradThreads) * kUnit - off, vocab, -INFINITY, v[j]);
+    for (int j = 0; j < kGradUnits; ++j) raw[j] = load_row_unit<T, kAligned>(x, c0 + j * kGradThreads * kUnit, vocab, -INFINITY);
   }
 #pragma unroll
   for (int j = 0; j < kGradUnits; ++j) {
-    const int64_t c = static_cast<int64_t>(u0 + j * kGradThreads) * kUnit - off;
+    const uint32_t c = c0 + j * kGradThreads * kUnit;
+    float v[kUnit];
+    if (zero) {
 #pragma unroll
-    for (int k = 0; k < kUnit; ++k) {
-      if (zero) {
-        v[j][k] = 0.f;
-      } else {
-        const float y = max_nan((v[j][k] - lse) * kLog2e, kTiny);
-        v[j][k] = exp2_fast(y) * fmaf(-c1, y, c0);
-        if (c + k == token) v[j][k] += g_lp;
+      for (int k = 0; k < kUnit; ++k) v[k] = 0.f;
+    } else {
+      unit_floats(raw[j], v);
+#pragma unroll
+      for (int k = 0; k < kUnit; k += 2) {
+        float2 y = mul2(add2(make_float2(v[k], v[k + 1]), make_float2(-lse, -lse)), make_float2(kLog2e, kLog2e));
+        y.x = max_nan(y.x, kTiny), y.y = max_nan(y.y, kTiny);
+        const float2 d = mul2(make_float2(exp2_fast(y.x), exp2_fast(y.y)), fma2(y, make_float2(-c1, -c1), make_float2(c0s, c0s)));
+        v[k] = d.x, v[k + 1] = d.y;
+      }
+      if (static_cast<uint64_t>(token - c) < kUnit) {
+#pragma unroll
+        for (int k = 0; k < kUnit; ++k) v[k] += c + k == token ? g_lp : 0.f;
       }
     }
-    store_values<T>(dx, c, vocab, v[j]);
+    store_row_unit<T, kAligned>(dx, c, vocab, v);
   }
 }
 
@@ -506,11 +511,11 @@ int launch_token_logprob(int dtype, const LogprobArgs& a, unsigned int* status, 
 
 int launch_token_logprob_grad(int dtype, const LogprobGradArgs& a, unsigned int* status, const LaunchShape& shape,
                               cudaStream_t stream) {
-  // one unit more than the row's: it may begin inside a 16-byte group
-  const uint32_t per_row = (a.vocab / kUnit + 2 + kGradThreads * kGradUnits - 1) / (kGradThreads * kGradUnits);
-  with_dtype(dtype, [&](auto t) {
+  const uint32_t per_row = ((a.vocab + kUnit - 1) / kUnit + kGradThreads * kGradUnits - 1) / (kGradThreads * kGradUnits);
+  const bool all = rows_aligned(dtype, a.logits, a.ld) && rows_aligned(dtype, a.dlogits, a.ld_d);
+  with_dtype_aligned(dtype, all, [&](auto t, auto aligned) {
     using T = decltype(t);
-    launch_lm(token_logprob_grad_kernel<T>, dim3(static_cast<unsigned>(a.rows * per_row)), kGradThreads, 0, 1, stream,
+    launch_lm(token_logprob_grad_kernel<T, decltype(aligned)::value>, dim3(static_cast<unsigned>(a.rows * per_row)), kGradThreads, 0, 1, stream,
               shape.chained, a, per_row, status);
   });
   return 1;

@@ -36,7 +36,7 @@ __device__ __forceinline__ void load_weights(const float* __restrict__ weight, u
   }
 }
 
-template <typename T, int kRowThreads, int kUnits>
+template <typename T, bool kAligned, int kRowThreads, int kUnits>
 __global__ void __launch_bounds__(kNormThreads<kRowThreads>)
 rmsnorm_pack_kernel(NormArgs a, ActView act, unsigned int* __restrict__ status) {
   constexpr int kRows = kNormThreads<kRowThreads> / kRowThreads;
@@ -49,12 +49,12 @@ rmsnorm_pack_kernel(NormArgs a, ActView act, unsigned int* __restrict__ status) 
   const T* x = static_cast<const T*>(a.x) + row * a.ld_x;
   float v[kUnits][kUnit];
 #pragma unroll
-  for (int j = 0; j < kUnits; ++j) load_values<T>(x, (j * kRowThreads + t) * kUnit, cols, 0.f, v[j]);
+  for (int j = 0; j < kUnits; ++j) load_values<T, kAligned>(x, (j * kRowThreads + t) * kUnit, cols, 0.f, v[j]);
   if (a.residual) {
     const T* r = static_cast<const T*>(a.residual) + row * a.ld_r;
     float w[kUnits][kUnit];
 #pragma unroll
-    for (int j = 0; j < kUnits; ++j) load_values<T>(r, (j * kRowThreads + t) * kUnit, cols, 0.f, w[j]);
+    for (int j = 0; j < kUnits; ++j) load_values<T, kAligned>(r, (j * kRowThreads + t) * kUnit, cols, 0.f, w[j]);
 #pragma unroll
     for (int j = 0; j < kUnits; ++j)
 #pragma unroll
@@ -68,7 +68,7 @@ rmsnorm_pack_kernel(NormArgs a, ActView act, unsigned int* __restrict__ status) 
   if (a.h) {
     T* h = static_cast<T*>(a.h) + row * a.ld_h;
 #pragma unroll
-    for (int j = 0; j < kUnits; ++j) store_values<T>(h, (j * kRowThreads + t) * kUnit, cols, v[j]);
+    for (int j = 0; j < kUnits; ++j) store_row_unit<T, kAligned>(h, (j * kRowThreads + t) * kUnit, cols, v[j]);
   }
   const float rstd = 1.f / sqrtf(row_sum<kRowThreads>(sq, sm) / static_cast<float>(cols) + a.eps);
   if (t == 0) a.rstd[row] = rstd;
@@ -81,10 +81,11 @@ rmsnorm_pack_kernel(NormArgs a, ActView act, unsigned int* __restrict__ status) 
     for (int k = 0; k < kUnit; ++k) v[j][k] *= rstd;
     const uint32_t b = act_exponent(block_largest(v[j]));
     const uint2 codes = act_codes(v[j], b);
-    if (c >= padded) continue;
-    *reinterpret_cast<uint2*>(act.codes + row * act.ld_codes + c) = codes;
-    if ((t & 3) == 0) act.exps[row * act.ld_exps + c / kActBlock] = static_cast<uint8_t>(b);
-    bad |= b == kActNan;
+    if (c < padded) {
+      *reinterpret_cast<uint2*>(act.codes + row * act.ld_codes + c) = codes;
+      if ((t & 3) == 0) act.exps[row * act.ld_exps + c / kActBlock] = static_cast<uint8_t>(b);
+      bad |= b == kActNan;
+    }
     if (!a.y) continue;
     const float unit = act_unit(b);
     if (a.weight) {
@@ -96,7 +97,7 @@ rmsnorm_pack_kernel(NormArgs a, ActView act, unsigned int* __restrict__ status) 
 #pragma unroll
       for (int k = 0; k < kUnit; ++k) v[j][k] *= unit;
     }
-    store_values<T>(static_cast<T*>(a.y) + row * a.ld_y, c, cols, v[j]);
+    store_row_unit<T, kAligned>(static_cast<T*>(a.y) + row * a.ld_y, c, cols, v[j]);
   }
   if (bad) atomicOr(status, kFlagNonFinite);
 }
@@ -110,9 +111,23 @@ struct NormRuns {
   uint32_t rows_per_run;
 };
 
+// What a thread holds of a row.  With one unit a thread the next row's is on its way while one is worked on; with
+// more there is no room for that, and the weights and dres are read where they are used.
+template <typename T, int kUnits> struct GradRow {
+  Unit<T> dy[kUnits], dres;
+  uint2 codes[kUnits];
+  uint32_t exps[kUnits];
+  float rstd;
+};
+
+// 64 registers, 80 for fp32 where the CTAs are small enough, 128 for the widest rows.
 template <typename T, int kRowThreads, int kUnits>
-__global__ void __launch_bounds__(kNormThreads<kRowThreads>)
-rmsnorm_grad_kernel(NormGradArgs a, ActView act, const __grid_constant__ NormRuns runs) {
+constexpr int kGradThreadsPerSm = kUnits > 1 ? kRowThreads : sizeof(T) == 4 && kRowThreads < 512 ? 768 : 1024;
+
+template <typename T, bool kAligned, int kRowThreads, int kUnits>
+__global__ void __launch_bounds__(kNormThreads<kRowThreads>, kGradThreadsPerSm<T, kRowThreads, kUnits> / kNormThreads<kRowThreads>)
+rmsnorm_grad_kernel(const __grid_constant__ NormGradArgs a, const __grid_constant__ ActView act,
+                    const __grid_constant__ NormRuns runs) {
   constexpr int kRows = kNormThreads<kRowThreads> / kRowThreads;
   constexpr int kCols = kRowThreads * kUnits * kUnit;
   __shared__ float sm[2][32];
@@ -125,58 +140,89 @@ rmsnorm_grad_kernel(NormGradArgs a, ActView act, const __grid_constant__ NormRun
   const uint32_t padded = (cols + kActBlock - 1) & ~static_cast<uint32_t>(kActBlock - 1);
   chain_wait();
   chain_trigger();
-  float w[kUnits][kUnit], dw[kUnits][kUnit];
+  constexpr bool kAhead = kUnits == 1;
+  float kept[kUnit], dw[kUnits][kUnit];
+  auto weights = [&](int j, float (&w)[kUnit]) {
+    if (a.weight) {
+      load_weights(a.weight, (j * kRowThreads + t) * kUnit, cols, w);
+    } else {
 #pragma unroll
-  for (int j = 0; j < kUnits; ++j) {
-    if (a.weight) load_weights(a.weight, (j * kRowThreads + t) * kUnit, cols, w[j]);
-#pragma unroll
-    for (int k = 0; k < kUnit; ++k) {
-      if (!a.weight) w[j][k] = 1.f;
-      dw[j][k] = 0.f;
+      for (int k = 0; k < kUnit; ++k) w[k] = 1.f;
     }
-  }
-  int turn = 0;
-  for (uint64_t row = first + sub; row < last; row += kRows, turn ^= 1) {
+  };
+  if (kAhead) weights(0, kept);
+#pragma unroll
+  for (int j = 0; j < kUnits; ++j)
+#pragma unroll
+    for (int k = 0; k < kUnit; ++k) dw[j][k] = 0.f;
+  auto load = [&](uint64_t row, GradRow<T, kUnits>& g) {
     const T* dy = static_cast<const T*>(a.dy) + row * a.ld_dy;
-    float n[kUnits][kUnit], u[kUnits][kUnit];
+    const T* dres = static_cast<const T*>(a.dres) + row * a.ld_dres;
+    g.rstd = a.rstd[row];
+#pragma unroll
+    for (int j = 0; j < kUnits; ++j) {
+      const uint32_t c = (j * kRowThreads + t) * kUnit;
+      g.dy[j] = load_row_unit<T, kAligned>(dy, c, cols, 0.f);
+      if (kAhead && a.dres) g.dres = load_row_unit<T, kAligned>(dres, c, cols, 0.f);
+      g.codes[j] = make_uint2(0u, 0u);
+      g.exps[j] = 7u;
+      if (c < padded) {
+        g.codes[j] = __ldcs(reinterpret_cast<const uint2*>(act.codes + row * act.ld_codes + c));
+        g.exps[j] = act.exps[row * act.ld_exps + c / kActBlock];
+      }
+    }
+  };
+  auto work = [&](uint64_t row, const GradRow<T, kUnits>& g, int turn) {
     float dot = 0.f;
 #pragma unroll
     for (int j = 0; j < kUnits; ++j) {
-      const uint32_t c = (j * kRowThreads + t) * kUnit;
-      load_values<T>(dy, c, cols, 0.f, u[j]);
-      uint2 codes = make_uint2(0u, 0u);
-      uint32_t b = 7u;
-      if (c < padded) {
-        codes = __ldcs(reinterpret_cast<const uint2*>(act.codes + row * act.ld_codes + c));
-        b = act.exps[row * act.ld_exps + c / kActBlock];
-      }
-      code_floats(codes, n[j]);
-      const float unit = act_unit(b);
-#pragma unroll
-      for (int k = 0; k < kUnit; ++k) n[j][k] *= unit;
-    }
-#pragma unroll
-    for (int j = 0; j < kUnits; ++j)
+      float u[kUnit], n[kUnit], w[kUnit];
+      unit_floats(g.dy[j], u);
+      code_floats(g.codes[j], n);
+      if (!kAhead) weights(j, w);
+      const float unit = act_unit(g.exps[j]);
 #pragma unroll
       for (int k = 0; k < kUnit; ++k) {
-        dw[j][k] = fmaf(u[j][k], n[j][k], dw[j][k]);
-        u[j][k] *= w[j][k];
-        dot = fmaf(u[j][k], n[j][k], dot);
+        n[k] *= unit;
+        const float un = u[k] * n[k];
+        dw[j][k] += un;
+        dot = fmaf(un, kAhead ? kept[k] : w[k], dot);
       }
-    const float mean = row_sum<kRowThreads>(dot, sm[turn]) / static_cast<float>(cols), rstd = a.rstd[row];
+    }
+    const float mean = row_sum<kRowThreads>(dot, sm[turn]) / static_cast<float>(cols), scale = -mean;
 #pragma unroll
     for (int j = 0; j < kUnits; ++j) {
       const uint32_t c = (j * kRowThreads + t) * kUnit;
-      if (c >= cols) continue;
+      float u[kUnit], n[kUnit], w[kUnit];
+      unit_floats(g.dy[j], u);
+      code_floats(g.codes[j], n);
+      if (!kAhead) weights(j, w);
+      const float unit = act_unit(g.exps[j]) * scale;
 #pragma unroll
-      for (int k = 0; k < kUnit; ++k) u[j][k] = rstd * fmaf(-n[j][k], mean, u[j][k]);
+      for (int k = 0; k < kUnit; ++k) u[k] = g.rstd * fmaf(n[k], unit, u[k] * (kAhead ? kept[k] : w[k]));
       if (a.dres) {
         float r[kUnit];
-        load_values<T>(static_cast<const T*>(a.dres) + row * a.ld_dres, c, cols, 0.f, r);
+        if (kAhead) unit_floats(g.dres, r);
+        else load_values<T, kAligned>(static_cast<const T*>(a.dres) + row * a.ld_dres, c, cols, 0.f, r);
 #pragma unroll
-        for (int k = 0; k < kUnit; ++k) u[j][k] += r[k];
+        for (int k = 0; k < kUnit; ++k) u[k] += r[k];
       }
-      store_values<T>(static_cast<T*>(a.dx) + row * a.ld_dx, c, cols, u[j]);
+      store_row_unit<T, kAligned>(static_cast<T*>(a.dx) + row * a.ld_dx, c, cols, u);
+    }
+  };
+  uint64_t row = first + sub;
+  if (row < last) {
+    GradRow<T, kUnits> one, two;
+    load(row, one);
+    for (;;) {
+      if (kAhead && row + kRows < last) load(row + kRows, two);
+      work(row, one, 0);
+      if ((row += kRows) >= last) break;
+      if (!kAhead) load(row, two);
+      if (kAhead && row + kRows < last) load(row + kRows, one);
+      work(row, two, 1);
+      if ((row += kRows) >= last) break;
+      if (!kAhead) load(row, one);
     }
   }
   if (!a.gw) return;
@@ -197,7 +243,7 @@ rmsnorm_grad_kernel(NormGradArgs a, ActView act, const __grid_constant__ NormRun
 #pragma unroll
     for (int j = 0; j < kUnits; ++j) {
       const uint32_t c = (j * kRowThreads + t) * kUnit;
-      if (c < cols) store_unit<float>(part + c, dw[j]);  // rows of partials are whole units
+      if (c < cols) store_unit(part + c, pack_unit<float>(dw[j]));  // rows of partials are whole units
     }
   }
 }
@@ -227,8 +273,6 @@ run_sum_kernel(const float* __restrict__ partials, const __grid_constant__ NormR
 }
 
 // ------------------------------------------------------------------ launchers
-// f(kRowThreads, kUnits) for a row of `cols` columns: the fewest threads that hold the row in at most four units
-// each.
 template <typename F> static void with_row(uint32_t cols, F f) {
   using std::integral_constant;
   if (cols <= 256) f(integral_constant<int, 32>(), integral_constant<int, 1>());
@@ -238,15 +282,27 @@ template <typename F> static void with_row(uint32_t cols, F f) {
   else if (cols <= 8192) f(integral_constant<int, 512>(), integral_constant<int, 2>());
   else f(integral_constant<int, 512>(), integral_constant<int, 4>());  // up to kNormMaxCols
 }
+// The gradient keeps a column's sum and weight beside two rows: one unit a thread.
+template <typename F> static void with_grad_row(uint32_t cols, F f) {
+  using std::integral_constant;
+  if (cols <= 256) f(integral_constant<int, 32>(), integral_constant<int, 1>());
+  else if (cols <= 1024) f(integral_constant<int, 128>(), integral_constant<int, 1>());
+  else if (cols <= 2048) f(integral_constant<int, 256>(), integral_constant<int, 1>());
+  else if (cols <= 4096) f(integral_constant<int, 512>(), integral_constant<int, 1>());
+  else if (cols <= 8192) f(integral_constant<int, 1024>(), integral_constant<int, 1>());
+  else f(integral_constant<int, 512>(), integral_constant<int, 4>());  // up to kNormMaxCols
+}
 
 int launch_rmsnorm_pack(int dtype, const NormArgs& a, const ActView& act, unsigned int* status, const LaunchShape& shape,
                         cudaStream_t stream) {
-  with_dtype(dtype, [&](auto t) {
+  const bool all = rows_aligned(dtype, a.x, a.ld_x) && (!a.residual || rows_aligned(dtype, a.residual, a.ld_r)) &&
+                   (!a.h || rows_aligned(dtype, a.h, a.ld_h)) && (!a.y || rows_aligned(dtype, a.y, a.ld_y));
+  with_dtype_aligned(dtype, all, [&](auto t, auto aligned) {
     using T = decltype(t);
     with_row(act.cols, [&](auto row_threads, auto units) {
       constexpr int kThreadsRow = decltype(row_threads)::value;
       constexpr unsigned kRows = kNormThreads<kThreadsRow> / kThreadsRow;
-      launch_lm(rmsnorm_pack_kernel<T, kThreadsRow, decltype(units)::value>,
+      launch_lm(rmsnorm_pack_kernel<T, decltype(aligned)::value, kThreadsRow, decltype(units)::value>,
                 dim3(static_cast<unsigned>((act.rows + kRows - 1) / kRows)), kNormThreads<kThreadsRow>, 0, 1, stream,
                 shape.chained, a, act, status);
     });
@@ -254,9 +310,12 @@ int launch_rmsnorm_pack(int dtype, const NormArgs& a, const ActView& act, unsign
   return 1;
 }
 
-// Runs of rows: about one per resident CTA, at most kNormRuns, plus what the workers' ends add.
-constexpr uint32_t kNormRuns = 592, kNormRunsWide = 296;  // rows of up to 4096 columns, wider ones
-static uint32_t norm_runs(uint32_t cols) { return cols <= 4096 ? kNormRuns : kNormRunsWide; }
+// Runs of rows: about one for each CTA that 148 SMs hold, plus what the workers' ends add.
+static uint32_t norm_runs(uint32_t cols) {
+  uint32_t runs = 0;
+  with_grad_row(cols, [&](auto row_threads, auto) { runs = 148u * (1024u / kNormThreads<decltype(row_threads)::value>); });
+  return runs;
+}
 uint64_t rmsnorm_grad_scratch_bytes(uint64_t cols, uint32_t M) {
   return (norm_runs(static_cast<uint32_t>(cols)) + M) * ((cols + 7) & ~7ull) * sizeof(float);
 }
@@ -267,18 +326,20 @@ int launch_rmsnorm_grad(int dtype, const NormGradArgs& a, const ActView& act, co
   runs.shards = shards;
   const uint64_t rows = shards.row0[a.M] - shards.row0[0], most = norm_runs(act.cols);
   runs.rows_per_run = static_cast<uint32_t>((rows + most - 1) / most);
-  if (act.cols <= 1024) runs.rows_per_run = (runs.rows_per_run + 7) / 8 * 8;  // eight rows at a time
+  if (act.cols <= 256) runs.rows_per_run = (runs.rows_per_run + 7) / 8 * 8;  // eight rows at a time
   if (!runs.rows_per_run) runs.rows_per_run = 1;
   runs.run0[0] = 0;
   for (uint32_t m = 0; m < a.M; ++m)
     runs.run0[m + 1] = runs.run0[m] + static_cast<uint32_t>((shards.row0[m + 1] - shards.row0[m] + runs.rows_per_run - 1) / runs.rows_per_run);
   int launches = 0;
   if (runs.run0[a.M]) {
-    with_dtype(dtype, [&](auto t) {
+    const bool all = rows_aligned(dtype, a.dy, a.ld_dy) && (!a.dres || rows_aligned(dtype, a.dres, a.ld_dres)) &&
+                     rows_aligned(dtype, a.dx, a.ld_dx);
+    with_dtype_aligned(dtype, all, [&](auto t, auto aligned) {
       using T = decltype(t);
-      with_row(act.cols, [&](auto row_threads, auto units) {
+      with_grad_row(act.cols, [&](auto row_threads, auto units) {
         constexpr int kThreadsRow = decltype(row_threads)::value;
-        launch_lm(rmsnorm_grad_kernel<T, kThreadsRow, decltype(units)::value>, dim3(runs.run0[a.M]),
+        launch_lm(rmsnorm_grad_kernel<T, decltype(aligned)::value, kThreadsRow, decltype(units)::value>, dim3(runs.run0[a.M]),
                   kNormThreads<kThreadsRow>, 0, 1, stream, shape.chained, a, act, runs);
       });
     });
