@@ -249,6 +249,7 @@ struct WgradArgs {
   void* scratch;
   uint64_t scratch_bytes, ld_dy, ld_g, ld_w;
   uint32_t out_cols, M;
+  int device;
   bool accumulate;
 };
 uint64_t act_wgrad_scratch_bytes(uint64_t out_cols, uint64_t cols, uint32_t M);

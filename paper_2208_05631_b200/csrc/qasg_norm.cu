@@ -20,6 +20,7 @@ __device__ __forceinline__ float row_sum(float v, float* sm) {
   constexpr int kWarps = kRowThreads / 32;
   if ((threadIdx.x & 31) == 0) sm[threadIdx.x >> 5] = v;
   __syncthreads();
+  if (kWarps > 8) return warp_sum((threadIdx.x & 31) < kWarps ? sm[threadIdx.x & 31] : 0.f);
   float s = 0.f;
 #pragma unroll
   for (int i = 0; i < kWarps; ++i) s += sm[i];
@@ -329,8 +330,12 @@ int launch_rmsnorm_grad(int dtype, const NormGradArgs& a, const ActView& act, co
   if (act.cols <= 256) runs.rows_per_run = (runs.rows_per_run + 7) / 8 * 8;  // eight rows at a time
   if (!runs.rows_per_run) runs.rows_per_run = 1;
   runs.run0[0] = 0;
-  for (uint32_t m = 0; m < a.M; ++m)
-    runs.run0[m + 1] = runs.run0[m] + static_cast<uint32_t>((shards.row0[m + 1] - shards.row0[m] + runs.rows_per_run - 1) / runs.rows_per_run);
+  for (;;) {  // the workers' last runs are short: not one run more than there is room for
+    for (uint32_t m = 0; m < a.M; ++m)
+      runs.run0[m + 1] = runs.run0[m] + static_cast<uint32_t>((shards.row0[m + 1] - shards.row0[m] + runs.rows_per_run - 1) / runs.rows_per_run);
+    if (runs.run0[a.M] <= most || runs.rows_per_run >= rows) break;
+    runs.rows_per_run += act.cols <= 256 ? 8 : 1 + runs.rows_per_run / 64;
+  }
   int launches = 0;
   if (runs.run0[a.M]) {
     const bool all = rows_aligned(dtype, a.dy, a.ld_dy) && (!a.dres || rows_aligned(dtype, a.dres, a.ld_dres)) &&

@@ -23,6 +23,8 @@
 // are pairs for it, whose sums go to scratch and are added in order by a second launch.
 #include <cuda.h>
 
+#include <atomic>
+
 #include "qasg_lm.cuh"
 
 namespace qasg {
@@ -672,16 +674,22 @@ int launch_act_wgrad(int dtype, const WgradArgs& a, const ActView& act, const Ro
   }
   if (!ok) return -1;
   const dim3 grid(2 * min(pairs, plan.units));
-  auto go = [&](auto kernel, uint32_t smem) {
-    cudaFuncAttributes attributes;
-    ok &= cudaFuncGetAttributes(&attributes, kernel) == cudaSuccess && attributes.numRegs == kLaunchRegs;
-    ok &= cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) == cudaSuccess;
+  auto go = [&](auto which, auto kernel, uint32_t smem) {
+    (void)which;  // its type makes this body, and its static, one for each kernel
+    static std::atomic<uint64_t> prepared{0};  // devices on which this kernel has its shared memory
+    const uint64_t device = 1ull << (a.device & 63);
+    if (!(prepared.load() & device)) {
+      cudaFuncAttributes attributes;
+      ok &= cudaFuncGetAttributes(&attributes, kernel) == cudaSuccess && attributes.numRegs == kLaunchRegs;
+      ok &= cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) == cudaSuccess;
+      if (ok) prepared.fetch_or(device);
+    }
     if (ok) launch_lm(kernel, grid, kWgThreads, smem, 1, stream, shape.chained, map_dy, map_codes, map_exps, plan, a, act.cols, status);
   };
-  if (tma) go(act_wgrad_kernel<__nv_bfloat16, true>, kWgSmem<1>);
-  else if (dtype == kDtypeBf16) go(act_wgrad_kernel<__nv_bfloat16, false>, kWgSmem<1>);
-  else if (dtype == kDtypeF16) go(act_wgrad_kernel<__half, false>, kWgSmem<2>);
-  else go(act_wgrad_kernel<float, false>, kWgSmem<3>);
+  if (tma) go(std::integral_constant<int, 0>(), act_wgrad_kernel<__nv_bfloat16, true>, kWgSmem<1>);
+  else if (dtype == kDtypeBf16) go(std::integral_constant<int, 1>(), act_wgrad_kernel<__nv_bfloat16, false>, kWgSmem<1>);
+  else if (dtype == kDtypeF16) go(std::integral_constant<int, 2>(), act_wgrad_kernel<__half, false>, kWgSmem<2>);
+  else go(std::integral_constant<int, 3>(), act_wgrad_kernel<float, false>, kWgSmem<3>);
   if (!ok) return -1;
   if (plan.pieces == 1) return 1;
   launch_lm(piece_sum_kernel, dim3((tiles - plan.whole) * 32), 256, 0, 1, stream, shape.chained, plan, a, act.cols);
