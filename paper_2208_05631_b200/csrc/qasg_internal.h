@@ -250,6 +250,7 @@ struct WgradArgs {
   uint64_t scratch_bytes, ld_dy, ld_g, ld_w;
   uint32_t out_cols, M;
   int device;
+  int vector;  // floats of g that lie aligned together: 4, 2 or 1; set by the launcher
   bool accumulate;
 };
 uint64_t act_wgrad_scratch_bytes(uint64_t out_cols, uint64_t cols, uint32_t M);

@@ -45,11 +45,11 @@ constexpr uint32_t kOperandBytes = kWgRows * kWgHalf * 2;  // 16 KB: two swizzle
 constexpr uint32_t kCodeBytes = kWgRows * kWgHalf;
 constexpr uint32_t kCodeStage = kCodeBytes + kWgRows * 16;  // and 16 exponent bytes a row
 constexpr uint32_t kAtomBytes = kWgRows * 128;             // 64 columns x 64 rows
-constexpr int kTurnCols = 16, kTurnPitch = 17;
+constexpr int kTurnCols = 16, kTurnPitch = 20;  // floats: rows of whole 16-byte words over all banks
 constexpr long long kMaxWait = 1ll << 34;                  // bound of every wait in cycles (some seconds)
 
-// How dy reaches shared memory: bf16 rows on 16-byte boundaries by TMA, everything else through the converting
-// warps' registers, as 1, 2 or 3 bf16 pieces.
+// How dy reaches shared memory, as 1, 2 or 3 bf16 pieces: 16-bit rows on 16-byte boundaries by TMA (fp16 is then split
+// in place by the converting warps), everything else through those warps' registers.
 template <typename T> constexpr int kPieces = 1;
 template <> constexpr int kPieces<__half> = 2;
 template <> constexpr int kPieces<float> = 3;
@@ -60,7 +60,7 @@ template <int kP> constexpr uint32_t kStageBytes = (kP + 1) * kOperandBytes;
 template <int kP> constexpr uint32_t kWgSmem = kStages<kP> * kStageBytes<kP> + kCodeStages * kCodeStage + 8 * 32 * kTurnPitch * 4 + 1024;
 
 struct WgradPlan {
-  RowShards shards;
+  uint32_t row0[kMaxWorkers + 1];
   uint32_t order[kMaxWorkers];  // workers, most rows first
   uint32_t tiles_n, tiles_k;    // per worker
   uint32_t whole;               // tiles summed by one pair each; the tiles after them are cut into pieces
@@ -176,7 +176,7 @@ template <int n> struct Ring {
 
 // ------------------------------------------------------------------ units of work
 struct TileWork {
-  uint64_t row0, row1;  // rows t
+  uint32_t row0, row1;  // rows t
   uint32_t worker, n0, k0;
   int32_t slot;         // the piece's place in scratch, -1: the outputs are final
 };
@@ -190,15 +190,19 @@ __device__ __forceinline__ TileWork unit_of(const WgradPlan& p, uint32_t u) {
   const uint32_t per_worker = p.tiles_n * p.tiles_k, w = tile / per_worker, i = tile - w * per_worker;
   // tiles in strips of eight rows of tiles, so that the pairs at work share operands in L2
   const uint32_t strip = i / (8 * p.tiles_k), high = min(8u, p.tiles_n - 8 * strip), j = i - strip * 8 * p.tiles_k;
+  const uint32_t across = j / high;
   TileWork r;
   r.worker = p.order[w];
-  r.n0 = (8 * strip + j % high) * kWgTile;
-  r.k0 = (j / high) * kWgTile;
-  const uint64_t first = p.shards.row0[r.worker], steps = (p.shards.row0[r.worker + 1] - first + kWgRows - 1) / kWgRows;
-  r.row0 = first + steps * piece / pieces * kWgRows;
-  r.row1 = min(first + steps * (piece + 1) / pieces * kWgRows, p.shards.row0[r.worker + 1]);
-  if (r.row0 > r.row1) r.row0 = r.row1;
-  r.slot = pieces > 1 ? static_cast<int32_t>(u - p.whole) : -1;
+  r.n0 = (8 * strip + j - across * high) * kWgTile;
+  r.k0 = across * kWgTile;
+  const uint32_t first = p.row0[r.worker], end = p.row0[r.worker + 1];
+  r.row0 = first, r.row1 = end, r.slot = -1;
+  if (pieces > 1) {  // whole stages; at most 2^25 of them times kMaxPairs
+    const uint32_t steps = (end - first + kWgRows - 1) / kWgRows;
+    r.row0 = min(first + steps * piece / pieces * kWgRows, end);
+    r.row1 = min(first + steps * (piece + 1) / pieces * kWgRows, end);
+    r.slot = static_cast<int32_t>(u - p.whole);
+  }
   return r;
 }
 
@@ -222,14 +226,17 @@ __device__ __forceinline__ uint4 code_octet(uint2 w, uint32_t two_e) {
   r.w = code_pair((y >> 8) & 0x00ff00ffu, two_e);
   return r;
 }
-// Column of a group of 16 that column i of the product holds.
-__device__ __forceinline__ constexpr int product_column(int i) { return (i & ~3) | ((i & 1) << 1) | ((i >> 1) & 1); }
 // Place of 16-byte chunk `chunk` (eight columns) of row t in an operand.
 __device__ __forceinline__ uint32_t chunk_offset(uint32_t t, uint32_t chunk) {
   return (chunk >> 3) * kAtomBytes + t * 128 + (((chunk & 7u) ^ (t & 7u)) << 4);
 }
 __device__ __forceinline__ void store_shared(uint32_t addr, uint4 v) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+__device__ __forceinline__ uint4 load_shared(uint32_t addr) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+  return v;
 }
 __device__ __forceinline__ uint2 load_shared2(uint32_t addr) {
   uint2 v;
@@ -240,6 +247,67 @@ __device__ __forceinline__ uint32_t load_shared1(uint32_t addr) {
   uint32_t v;
   asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
   return v;
+}
+
+// A warp's sums (lane = row) to `rows` x `width` outputs, 16 columns at a time turned in shared memory so that kVector
+// floats leave in one store (the outputs' rows are aligned to that), 64 bytes of a row beside one another.  What an SM
+// can send out bounds this: about 13 bytes a cycle, 10,000 cycles for its half of a tile, whatever the stores' width.
+template <int kVector, bool kAdd>
+__device__ __forceinline__ void store_sums(float* turn, uint32_t lane, const float (&sum)[kWgHalf], float* out, uint64_t pitch,
+                                           uint32_t width, uint32_t rows, const float* weight) {
+  constexpr int kAcross = kTurnCols / kVector, kDown = 32 / kAcross;  // lanes of a row, rows of a store
+  const uint32_t r = lane / kAcross, c = lane % kAcross * kVector;
+#pragma unroll
+  for (int i = 0; i < kWgHalf / kTurnCols; ++i) {
+    float by[kVector];
+#pragma unroll
+    for (int j = 0; j < kVector; ++j) by[j] = weight && i * kTurnCols + c + j < width ? __ldg(weight + i * kTurnCols + c + j) : 1.f;
+    __syncwarp();
+#pragma unroll
+    for (int j = 0; j < kTurnCols; j += 4)  // the products' columns stand in the order 0 2 1 3
+      *reinterpret_cast<float4*>(turn + lane * kTurnPitch + j) =
+          make_float4(sum[i * kTurnCols + j], sum[i * kTurnCols + j + 2], sum[i * kTurnCols + j + 1], sum[i * kTurnCols + j + 3]);
+    __syncwarp();
+    float v[32 / kDown][kVector];
+#pragma unroll
+    for (int d = 0; d < 32 / kDown; ++d)
+#pragma unroll
+      for (int j = 0; j < kVector; ++j) v[d][j] = turn[(d * kDown + r) * kTurnPitch + c + j] * by[j];
+    const uint32_t at = i * kTurnCols + c;
+    if (at >= width) continue;
+    float* to = out + r * pitch + at;
+#pragma unroll
+    for (int d = 0; d < 32 / kDown; ++d, to += kDown * pitch) {
+      if (d * kDown + r >= rows) break;
+      if (kVector == 1) {
+        *to = kAdd ? *to + v[d][0] : v[d][0];
+      } else if (at + kVector <= width) {
+        if (kVector == 4) *reinterpret_cast<float4*>(to) = make_float4(v[d][0], v[d][1], v[d][kVector - 2], v[d][kVector - 1]);
+        else *reinterpret_cast<float2*>(to) = make_float2(v[d][0], v[d][kVector - 1]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < kVector; ++j)
+          if (at + j < width) to[j] = v[d][j];
+      }
+    }
+  }
+}
+
+// The leading eight bits of eight values as bf16; v becomes what is left (nothing of an infinity).
+__device__ __forceinline__ uint4 leading_bits(float (&v)[kUnit]) {
+  uint32_t q[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) q[j] = __byte_perm(__float_as_uint(v[2 * j]), __float_as_uint(v[2 * j + 1]), 0x7632);
+  float largest = fabsf(v[0]);
+#pragma unroll
+  for (int j = 1; j < kUnit; ++j) largest = max_nan(largest, fabsf(v[j]));
+  const bool finite = largest < INFINITY;
+#pragma unroll
+  for (int j = 0; j < kUnit; ++j) {
+    const float rest = v[j] - __uint_as_float(__float_as_uint(v[j]) & 0xffff0000u);
+    v[j] = finite || fabsf(v[j]) < INFINITY ? rest : 0.f;
+  }
+  return make_uint4(q[0], q[1], q[2], q[3]);
 }
 
 // The raw words of columns [c, c + 8) of a row of n values, zeros past its end; any alignment.
@@ -287,7 +355,7 @@ act_wgrad_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_consta
     gave_up = 0u;
     for (int s = 0; s < kN; ++s) {
       barrier_init(full + 8 * s, 1);
-      barrier_init(ready + 8 * s, 2 * kGroupWarps + (kTma ? 2 : 0));
+      barrier_init(ready + 8 * s, 2 * kGroupWarps + (kTma && kP == 1 ? 2 : 0));
       barrier_init(empty + 8 * s, 1);
     }
     for (int s = 0; s < kCodeStages; ++s) {
@@ -299,6 +367,11 @@ act_wgrad_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_consta
       barrier_init(acc_empty + 8 * i, 16);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (tid == 32) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&map_dy) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&map_codes) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&map_exps) : "memory");
   }
   if (warp == 2) {
     asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&tmem_base)) : "memory");
@@ -324,7 +397,7 @@ act_wgrad_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_consta
       for (uint32_t u = pair; u < plan.units && ok; u += pairs) {
         const TileWork w = unit_of(plan, u);
         const int n = static_cast<int>(w.n0 + rank * kWgHalf), k = static_cast<int>(w.k0 + rank * kWgHalf);
-        for (uint32_t y = static_cast<uint32_t>(w.row0); y < static_cast<uint32_t>(w.row1); y += kWgRows) {
+        for (uint32_t y = w.row0; y < w.row1; y += kWgRows) {
           if (!(ok = all_wait(code_empty + 8 * rc.at, rc.phase ^ 1u, &gave_up))) break;
           if (one) {
             const uint32_t bar = code_full + 8 * rc.at, at = at_codes + rc.at * kCodeStage;
@@ -365,7 +438,7 @@ act_wgrad_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_consta
       bool ok = true;
       for (uint32_t u = pair; u < plan.units && ok; u += pairs) {
         const TileWork w = unit_of(plan, u);
-        uint32_t left = static_cast<uint32_t>((w.row1 - w.row0 + kWgRows - 1) / kWgRows);
+        uint32_t left = (w.row1 - w.row0 + kWgRows - 1) / kWgRows;
         if (rank != 0) {  // the first CTA issues; this one keeps count of the ring
           for (; left; --left) r.next();
           continue;
@@ -396,13 +469,13 @@ act_wgrad_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_consta
         }
       }
       if (lane == 0) last_at = r.at, last_phase = r.phase;
-    } else if (warp == 3 && kTma) {
+    } else if (warp == 3 && kTma && kP == 1) {
       Ring<kN> r = {0, 0};
       const uint32_t ready_of_first = map_rank(ready, 0);
       bool ok = true;
       for (uint32_t u = pair; u < plan.units && ok; u += pairs) {
         const TileWork w = unit_of(plan, u);
-        uint32_t rows = static_cast<uint32_t>(w.row1 - w.row0);
+        uint32_t rows = w.row1 - w.row0;
         while (rows) {
           if (!(ok = all_wait(full + 8 * r.at, r.phase, &gave_up))) break;
           if (rows < kWgRows) {  // rows of another worker came with the copy: they must not meet 0 * inf
@@ -439,15 +512,15 @@ act_wgrad_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_consta
       const TileWork w = unit_of(plan, u);
       const uint32_t exp_at = ((w.k0 + rank * kWgHalf) / kActBlock) & 15u;  // four blocks: one word
       const uint32_t n = w.n0 + rank * kWgHalf + chunk * kUnit;
-      for (uint64_t t = w.row0; t < w.row1; t += kWgRows, r.next(), rc.next(), turn ^= 1u) {
+      for (uint32_t t = w.row0; t < w.row1; t += kWgRows, r.next(), rc.next(), turn ^= 1u) {
         if (turn != group) continue;
-        const uint32_t rows = static_cast<uint32_t>(min(static_cast<uint64_t>(kWgRows), w.row1 - t));
+        const uint32_t rows = min(static_cast<uint32_t>(kWgRows), w.row1 - t);
         Unit<T> raw[kTma ? 1 : kLoads];
         auto load = [&](int batch) {
 #pragma unroll
           for (int i = 0; i < kLoads; ++i) {
             const uint32_t y = (ctid >> 4) + 8 * (batch * kLoads + i);
-            raw[kTma ? 0 : i] = load_raw<T>(dy + (t + y) * a.ld_dy, n, y < rows ? a.out_cols : 0u);
+            raw[kTma ? 0 : i] = load_raw<T>(dy + static_cast<uint64_t>(t + y) * a.ld_dy, n, y < rows ? a.out_cols : 0u);
           }
         };
         if (!kTma) load(0);
@@ -476,6 +549,21 @@ act_wgrad_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_consta
               store_shared(out + to1 + i * 2048, make_uint4(0u, 0u, 0u, 0u));
             }
         }
+        if (kTma && kP == 2) {
+          if (!(ok = all_wait(full + 8 * r.at, r.phase, &gave_up))) break;
+#pragma unroll 2
+          for (int i = 0; i < 8; ++i) {
+            const uint32_t y = (ctid >> 4) + 8 * i, at = stage + chunk_offset(y, chunk);
+            uint4 q = load_shared(at);
+            if (y >= rows) q = make_uint4(0u, 0u, 0u, 0u);  // rows of another worker came with the copy
+            Unit<T> u;
+            u.w[0] = q.x, u.w[1] = q.y, u.w[2] = q.z, u.w[3] = q.w;
+            float v[kUnit];
+            unit_floats(u, v);
+            store_shared(at, leading_bits(v));
+            store_shared(at + kOperandBytes, leading_bits(v));
+          }
+        }
         if (!kTma) {
           for (int batch = 0; batch < 8 / kLoads; ++batch) {
             if (batch) load(batch);
@@ -484,19 +572,8 @@ act_wgrad_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_consta
               float v[kUnit];
               unit_floats(raw[i], v);
 #pragma unroll
-              for (int p = 0; p < kP; ++p) {  // the leading eight bits as bf16, then those of what is left
-                uint32_t q[4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                  q[j] = __byte_perm(__float_as_uint(v[2 * j]), __float_as_uint(v[2 * j + 1]), 0x7632);
-#pragma unroll
-                for (int j = 0; j < kUnit; ++j) {
-                  const float rest = v[j] - __uint_as_float(__float_as_uint(v[j]) & 0xffff0000u);
-                  v[j] = fabsf(v[j]) < INFINITY ? rest : 0.f;
-                }
-                store_shared(stage + p * kOperandBytes + chunk_offset((ctid >> 4) + 8 * (batch * kLoads + i), chunk),
-                             make_uint4(q[0], q[1], q[2], q[3]));
-              }
+              for (int p = 0; p < kP; ++p)
+                store_shared(stage + p * kOperandBytes + chunk_offset((ctid >> 4) + 8 * (batch * kLoads + i), chunk), leading_bits(v));
             }
           }
         }
@@ -522,7 +599,7 @@ act_wgrad_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_consta
       float sum[kWgHalf];
 #pragma unroll
       for (int i = 0; i < kWgHalf; ++i) sum[i] = 0.f;
-      for (uint32_t left = static_cast<uint32_t>((w.row1 - w.row0 + kWgRows - 1) / kWgRows); left;
+      for (uint32_t left = (w.row1 - w.row0 + kWgRows - 1) / kWgRows; left;
            left -= min(left, static_cast<uint32_t>(kSegment))) {
         if (!(ok = all_wait(acc_full + 8 * acc.at, acc.phase, &gave_up))) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -541,32 +618,21 @@ act_wgrad_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_consta
         acc.next();
       }
       if (!ok) break;
-      const uint32_t row = rank * kWgHalf + quarter * 32 + (lane >> 4), col = half * kWgHalf + (lane & 15u);
-#pragma unroll
-      for (int c = 0; c < kWgHalf; c += kTurnCols) {
-        __syncwarp();
-#pragma unroll
-        for (int i = 0; i < kTurnCols; ++i) turn[lane * kTurnPitch + product_column(i)] = sum[c + i];
-        __syncwarp();
-        const float* from = turn + (lane >> 4) * kTurnPitch + (lane & 15u);
-        const uint32_t k = w.k0 + col + c, n = w.n0 + row;
-        if (w.slot >= 0) {
-          float* out = static_cast<float*>(a.scratch) + (static_cast<uint64_t>(w.slot) * kWgTile + row) * kWgTile + col + c;
-#pragma unroll 8
-          for (int i = 0; i < 16; ++i) out[2 * i * kWgTile] = from[2 * i * kTurnPitch];
-        } else if (k < cols && n < a.out_cols) {
-          const float scale = a.weight ? __ldg(a.weight + k) : 1.f;
-          float* out = a.g + w.worker * a.ld_g + n * a.ld_w + k;
-          const int rows = static_cast<int>(min(16u, (a.out_cols - n + 1) / 2));
-          if (a.accumulate) {
-#pragma unroll 4
-            for (int i = 0; i < rows; ++i) out[2 * i * a.ld_w] += from[2 * i * kTurnPitch] * scale;
-          } else {
-#pragma unroll 4
-            for (int i = 0; i < rows; ++i) out[2 * i * a.ld_w] = from[2 * i * kTurnPitch] * scale;
-          }
-        }
+      const uint32_t row = rank * kWgHalf + quarter * 32, col = half * kWgHalf;
+      if (w.slot >= 0) {
+        float* out = static_cast<float*>(a.scratch) + (static_cast<uint64_t>(w.slot) * kWgTile + row) * kWgTile + col;
+        store_sums<4, false>(turn, lane, sum, out, kWgTile, kWgHalf, 32, nullptr);
+        continue;
       }
+      const uint32_t n = w.n0 + row, k = w.k0 + col;
+      if (n >= a.out_cols || k >= cols) continue;
+      float* out = a.g + w.worker * a.ld_g + n * a.ld_w + k;
+      const float* weight = a.weight ? a.weight + k : nullptr;
+      const uint32_t width = min(static_cast<uint32_t>(kWgHalf), cols - k), rows = min(32u, a.out_cols - n);
+      if (a.accumulate) store_sums<1, true>(turn, lane, sum, out, a.ld_w, width, rows, weight);
+      else if (a.vector == 4) store_sums<4, false>(turn, lane, sum, out, a.ld_w, width, rows, weight);
+      else if (a.vector == 2) store_sums<2, false>(turn, lane, sum, out, a.ld_w, width, rows, weight);
+      else store_sums<1, false>(turn, lane, sum, out, a.ld_w, width, rows, weight);
     }
   }
   __syncwarp();
@@ -646,7 +712,7 @@ int launch_act_wgrad(int dtype, const WgradArgs& a, const ActView& act, const Ro
                      const LaunchShape& shape, cudaStream_t stream) {
   if (!encode_tiled()) return -1;
   WgradPlan plan;
-  plan.shards = shards;
+  for (uint32_t m = 0; m <= a.M; ++m) plan.row0[m] = static_cast<uint32_t>(shards.row0[m]);
   plan.tiles_n = (a.out_cols + kWgTile - 1) / kWgTile;
   plan.tiles_k = (act.cols + kWgTile - 1) / kWgTile;
   for (uint32_t m = 0; m < a.M; ++m) {  // most rows first: the short ones fill up the last round
@@ -663,12 +729,15 @@ int launch_act_wgrad(int dtype, const WgradArgs& a, const ActView& act, const Ro
   plan.whole = plan.pieces > 1 ? tiles - left : tiles;
   plan.units = plan.whole + plan.pieces * (tiles - plan.whole);
 
-  const bool tma = dtype == kDtypeBf16 && a.ld_dy % 8 == 0 && (reinterpret_cast<uintptr_t>(a.dy) & 15u) == 0;
+  WgradArgs args = a;
+  const uint64_t all = reinterpret_cast<uintptr_t>(a.g) / 4 | a.ld_w | (a.M > 1 ? a.ld_g : 0);
+  args.vector = all % 4 == 0 ? 4 : all % 2 == 0 ? 2 : 1;
+  const bool tma = dtype != kDtypeF32 && a.ld_dy % 8 == 0 && (reinterpret_cast<uintptr_t>(a.dy) & 15u) == 0;
   CUtensorMap map_dy = {}, map_codes = {}, map_exps = {};
   bool ok = true;
   if (act.rows) {  // without rows no copy is issued
     const uint32_t padded = (act.cols + kActBlock - 1) / kActBlock * kActBlock;
-    if (tma) ok &= make_map(&map_dy, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, a.dy, a.out_cols, act.rows, a.ld_dy, 64, true);
+    if (tma) ok &= make_map(&map_dy, dtype == kDtypeF16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, a.dy, a.out_cols, act.rows, a.ld_dy, 64, true);
     ok &= make_map(&map_codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, act.codes, padded, act.rows, act.ld_codes, kWgHalf, false);
     ok &= make_map(&map_exps, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, act.exps, act.ld_exps, act.rows, act.ld_exps, 16, false);
   }
@@ -684,9 +753,10 @@ int launch_act_wgrad(int dtype, const WgradArgs& a, const ActView& act, const Ro
       ok &= cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) == cudaSuccess;
       if (ok) prepared.fetch_or(device);
     }
-    if (ok) launch_lm(kernel, grid, kWgThreads, smem, 1, stream, shape.chained, map_dy, map_codes, map_exps, plan, a, act.cols, status);
+    if (ok) launch_lm(kernel, grid, kWgThreads, smem, 1, stream, shape.chained, map_dy, map_codes, map_exps, plan, args, act.cols, status);
   };
-  if (tma) go(std::integral_constant<int, 0>(), act_wgrad_kernel<__nv_bfloat16, true>, kWgSmem<1>);
+  if (tma && dtype == kDtypeBf16) go(std::integral_constant<int, 0>(), act_wgrad_kernel<__nv_bfloat16, true>, kWgSmem<1>);
+  else if (tma) go(std::integral_constant<int, 4>(), act_wgrad_kernel<__half, true>, kWgSmem<2>);
   else if (dtype == kDtypeBf16) go(std::integral_constant<int, 1>(), act_wgrad_kernel<__nv_bfloat16, false>, kWgSmem<1>);
   else if (dtype == kDtypeF16) go(std::integral_constant<int, 2>(), act_wgrad_kernel<__half, false>, kWgSmem<2>);
   else go(std::integral_constant<int, 3>(), act_wgrad_kernel<float, false>, kWgSmem<3>);
