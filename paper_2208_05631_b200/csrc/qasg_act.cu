@@ -38,16 +38,18 @@ act_pack_kernel(const T* __restrict__ x, uint64_t ld_x, ActView act, uint64_t it
   const ActItem a = act_item(item, per_row);
   const T* row = x + a.row * ld_x;
   const uint32_t padded = (act.cols + kActBlock - 1) & ~static_cast<uint32_t>(kActBlock - 1);
-  float v[kActItemUnits][kUnit];
+  const Extent tensor = extent_of(x, act.rows, ld_x, act.cols);
+  Fetched<T, kAligned> f[kActItemUnits];
 #pragma unroll
-  for (int j = 0; j < kActItemUnits; ++j)
-    load_values<T, kAligned>(row, a.col + (j * 32 + lane) * kUnit, act.cols, 0.f, v[j]);
+  for (int j = 0; j < kActItemUnits; ++j) f[j] = fetch_unit<T, kAligned>(row, a.row, a.col + (j * 32 + lane) * kUnit, act.cols, tensor);
   bool bad = false;
 #pragma unroll
   for (int j = 0; j < kActItemUnits; ++j) {
     const uint32_t c = a.col + (j * 32 + lane) * kUnit;
-    const uint32_t b = act_exponent(block_largest(v[j]));
-    const uint2 codes = act_codes(v[j], b);
+    float v[kUnit];
+    unit_floats(finish_unit(f[j], row, c, act.cols), v);
+    const uint32_t b = act_exponent(block_largest(v));
+    const uint2 codes = act_codes(v, b);
     if (c < padded) {
       *reinterpret_cast<uint2*>(act.codes + a.row * act.ld_codes + c) = codes;
       if ((lane & 3) == 0) act.exps[a.row * act.ld_exps + c / kActBlock] = static_cast<uint8_t>(b);

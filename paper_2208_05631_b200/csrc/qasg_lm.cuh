@@ -88,33 +88,76 @@ __device__ __forceinline__ void shifted_words(const uint32_t (&x)[kWords + 4], u
   for (int i = 0; i < kWords; ++i) out[i] = __funnelshift_r(z[i], z[i + 1], (shift & 2u) * 8);
 }
 
-// The unit at column c of a row of n values, `fill` past its end.  kAligned: every row begins on a 16-byte boundary.
-// Otherwise the aligned words around a unit are read and shifted, as long as those lie in the row too.
+// The first byte of a tensor and the one after its last: what may be read.  Eight rows from its ends (16 bytes at the
+// least) the aligned words around a row lie in it.
+struct Extent {
+  const char *lo, *hi;
+  uint64_t inner_rows;  // rows 8 to 8 + inner_rows - 1
+};
+template <typename T> __device__ __forceinline__ Extent extent_of(const T* base, uint64_t rows, uint64_t ld, uint64_t cols) {
+  return {reinterpret_cast<const char*>(base), reinterpret_cast<const char*>(base + (rows - 1) * ld + cols),
+          rows > 16 ? rows - 16 : 0};
+}
+
+// A unit on its way: fetch_unit() asks for the words, finish_unit() waits for them.  kAligned: every row begins on a
+// 16-byte boundary.  Otherwise the aligned words around the unit are read, the neighbours' bytes in them too where
+// they lie in the tensor, and finish_unit() shifts them.
+template <typename T, bool kAligned> struct Fetched { uint32_t w[kUnit * sizeof(T) / 4 + (kAligned ? 0 : 4)]; };
+
 template <typename T, bool kAligned>
-__device__ __forceinline__ Unit<T> load_row_unit(const T* row, uint32_t c, uint32_t n, float fill) {
-  constexpr uint32_t kWords = sizeof(Unit<T>) / 4;
-  const uint32_t shift = kAligned ? 0u : static_cast<uint32_t>(reinterpret_cast<uintptr_t>(row)) & 15u;
-  Unit<T> u;
-  if (shift == 0 && c + kUnit <= n) {
-    u = load_unit(row + c);
-  } else if (!kAligned && shift && c >= shift / sizeof(T) && c + kUnit + (16u - shift) / sizeof(T) <= n) {
-    const uint4* q = reinterpret_cast<const uint4*>(row + c - shift / sizeof(T));
-    uint32_t x[kWords + 4];
+__device__ __forceinline__ Fetched<T, kAligned> fetch_unit(const T* row, uint64_t index, uint32_t c, uint32_t n,
+                                                           const Extent& tensor) {
+  constexpr int kVectors = sizeof(Fetched<T, kAligned>) / 16;
+  Fetched<T, kAligned> f;
 #pragma unroll
-    for (uint32_t k = 0; k < kWords / 4 + 1; ++k) {
-      const uint4 v = q[k];
-      x[4 * k] = v.x, x[4 * k + 1] = v.y, x[4 * k + 2] = v.z, x[4 * k + 3] = v.w;
+  for (int i = 0; i < 4 * kVectors; ++i) f.w[i] = 0u;
+  if (c >= n) return f;
+  const char* from = reinterpret_cast<const char*>(row + c);
+  from -= kAligned ? 0 : reinterpret_cast<uintptr_t>(from) & 15u;
+  if (kAligned ? c + kUnit <= n : index - 8 < tensor.inner_rows) {
+#pragma unroll
+    for (int k = 0; k < kVectors; ++k) {
+      const uint4* q = reinterpret_cast<const uint4*>(from) + k;
+      const uint4 v = kAligned ? __ldcs(q) : *q;
+      f.w[4 * k] = v.x, f.w[4 * k + 1] = v.y, f.w[4 * k + 2] = v.z, f.w[4 * k + 3] = v.w;
     }
-    shifted_words<kWords>(x, shift, u.w);
-  } else {
+    return f;
+  }
 #pragma unroll
-    for (int k = 0; k < kUnit; ++k) set_value(u, k, c + k < n ? to_float(row[c + k]) : fill);
+  for (int k = 0; k < kVectors; ++k, from += 16) {
+    if (from >= tensor.lo && from + 16 <= tensor.hi) {
+      const uint4 v = *reinterpret_cast<const uint4*>(from);
+      f.w[4 * k] = v.x, f.w[4 * k + 1] = v.y, f.w[4 * k + 2] = v.z, f.w[4 * k + 3] = v.w;
+    } else {  // the tensor's first or last few values
+#pragma unroll
+      for (int i = 0; i < 16; i += sizeof(T)) {
+        if (from + i < tensor.lo || from + i >= tensor.hi) continue;
+        if (sizeof(T) == 4) f.w[4 * k + i / 4] = *reinterpret_cast<const uint32_t*>(from + i);
+        else f.w[4 * k + i / 4] |= static_cast<uint32_t>(*reinterpret_cast<const uint16_t*>(from + i)) << (8 * (i & 2));
+      }
+    }
+  }
+  return f;
+}
+// Zeros past the end of the row.
+template <typename T, bool kAligned>
+__device__ __forceinline__ Unit<T> finish_unit(const Fetched<T, kAligned>& f, const T* row, uint32_t c, uint32_t n) {
+  constexpr int kWords = sizeof(Unit<T>) / 4, kEach = 4 / sizeof(T);
+  Unit<T> u;
+  if constexpr (kAligned) {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) u.w[i] = f.w[i];
+  } else {
+    shifted_words<kWords>(f.w, static_cast<uint32_t>(reinterpret_cast<uintptr_t>(row)) & 15u, u.w);
+  }
+  if (c + kUnit > n) {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) {
+      if (c + i * kEach >= n) u.w[i] = 0u;
+      else if (kEach == 2 && c + i * kEach + 1 >= n) u.w[i] &= 0xffffu;
+    }
   }
   return u;
-}
-template <typename T, bool kAligned>
-__device__ __forceinline__ void load_values(const T* row, uint32_t c, uint32_t n, float fill, float (&v)[kUnit]) {
-  unit_floats(load_row_unit<T, kAligned>(row, c, n, fill), v);
 }
 
 template <typename T> __device__ __forceinline__ Unit<T> pack_unit(const float (&v)[kUnit]) {

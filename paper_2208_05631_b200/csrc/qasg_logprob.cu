@@ -459,10 +459,11 @@ token_logprob_grad_kernel(LogprobGradArgs a, uint32_t per_row, unsigned int* __r
   // p (c0s - c1 y) with y = log2 p
   const float c0s = g_lse - g_lp - (a.g_entropy ? g_h * a.entropy[row] : 0.f), c1 = g_h * kLn2;
   const uint32_t c0 = (part * (kGradThreads * kGradUnits) + threadIdx.x) * kUnit;
-  Unit<T> raw[kGradUnits];
+  const Extent tensor = extent_of(static_cast<const T*>(a.logits), a.rows, a.ld, vocab);
+  Fetched<T, kAligned> f[kGradUnits];
   if (!zero) {
 #pragma unroll
-    for (int j = 0; j < kGradUnits; ++j) raw[j] = load_row_unit<T, kAligned>(x, c0 + j * kGradThreads * kUnit, vocab, -INFINITY);
+    for (int j = 0; j < kGradUnits; ++j) f[j] = fetch_unit<T, kAligned>(x, row, c0 + j * kGradThreads * kUnit, vocab, tensor);
   }
 #pragma unroll
   for (int j = 0; j < kGradUnits; ++j) {
@@ -472,7 +473,7 @@ token_logprob_grad_kernel(LogprobGradArgs a, uint32_t per_row, unsigned int* __r
 #pragma unroll
       for (int k = 0; k < kUnit; ++k) v[k] = 0.f;
     } else {
-      unit_floats(raw[j], v);
+      unit_floats(finish_unit(f[j], x, c, vocab), v);
 #pragma unroll
       for (int k = 0; k < kUnit; k += 2) {
         float2 y = mul2(add2(make_float2(v[k], v[k + 1]), make_float2(-lse, -lse)), make_float2(kLog2e, kLog2e));

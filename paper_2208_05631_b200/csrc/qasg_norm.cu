@@ -48,18 +48,27 @@ rmsnorm_pack_kernel(NormArgs a, ActView act, unsigned int* __restrict__ status) 
   chain_trigger();
   if (kRows > 1 && row >= act.rows) return;  // whole warps: nothing meets below when a row is one warp
   const T* x = static_cast<const T*>(a.x) + row * a.ld_x;
+  const T* r = a.residual ? static_cast<const T*>(a.residual) + row * a.ld_r : nullptr;
+  Fetched<T, kAligned> fx[kUnits], fr[kUnits];
+  const Extent x_tensor = extent_of(static_cast<const T*>(a.x), act.rows, a.ld_x, cols);
+  const Extent r_tensor = extent_of(static_cast<const T*>(a.residual), act.rows, a.ld_r, cols);
+#pragma unroll
+  for (int j = 0; j < kUnits; ++j) {
+    const uint32_t c = (j * kRowThreads + t) * kUnit;
+    fx[j] = fetch_unit<T, kAligned>(x, row, c, cols, x_tensor);
+    if (r) fr[j] = fetch_unit<T, kAligned>(r, row, c, cols, r_tensor);
+  }
   float v[kUnits][kUnit];
 #pragma unroll
-  for (int j = 0; j < kUnits; ++j) load_values<T, kAligned>(x, (j * kRowThreads + t) * kUnit, cols, 0.f, v[j]);
-  if (a.residual) {
-    const T* r = static_cast<const T*>(a.residual) + row * a.ld_r;
-    float w[kUnits][kUnit];
+  for (int j = 0; j < kUnits; ++j) {
+    const uint32_t c = (j * kRowThreads + t) * kUnit;
+    unit_floats(finish_unit(fx[j], x, c, cols), v[j]);
+    if (r) {
+      float w[kUnit];
+      unit_floats(finish_unit(fr[j], r, c, cols), w);
 #pragma unroll
-    for (int j = 0; j < kUnits; ++j) load_values<T, kAligned>(r, (j * kRowThreads + t) * kUnit, cols, 0.f, w[j]);
-#pragma unroll
-    for (int j = 0; j < kUnits; ++j)
-#pragma unroll
-      for (int k = 0; k < kUnit; ++k) v[j][k] += w[j][k];
+      for (int k = 0; k < kUnit; ++k) v[j][k] += w[k];
+    }
   }
   float sq = 0.f;
 #pragma unroll
@@ -112,10 +121,10 @@ struct NormRuns {
   uint32_t rows_per_run;
 };
 
-// What a thread holds of a row.  With one unit a thread the next row's is on its way while one is worked on; with
-// more there is no room for that, and the weights and dres are read where they are used.
-template <typename T, int kUnits> struct GradRow {
-  Unit<T> dy[kUnits], dres;
+// What a thread holds of the next row while it works on one.  With more than one unit a thread there is no room for
+// that, and dres and the weights are read where they are used.
+template <typename T, bool kAligned, int kUnits> struct GradRow {
+  Fetched<T, kAligned> dy[kUnits], dres;
   uint2 codes[kUnits];
   uint32_t exps[kUnits];
   float rstd;
@@ -156,15 +165,17 @@ rmsnorm_grad_kernel(const __grid_constant__ NormGradArgs a, const __grid_constan
   for (int j = 0; j < kUnits; ++j)
 #pragma unroll
     for (int k = 0; k < kUnit; ++k) dw[j][k] = 0.f;
-  auto load = [&](uint64_t row, GradRow<T, kUnits>& g) {
-    const T* dy = static_cast<const T*>(a.dy) + row * a.ld_dy;
-    const T* dres = static_cast<const T*>(a.dres) + row * a.ld_dres;
+  const Extent dy_tensor = extent_of(static_cast<const T*>(a.dy), act.rows, a.ld_dy, cols);
+  const Extent dres_tensor = extent_of(static_cast<const T*>(a.dres), act.rows, a.ld_dres, cols);
+  auto dy_row = [&](uint64_t row) { return static_cast<const T*>(a.dy) + row * a.ld_dy; };
+  auto dres_row = [&](uint64_t row) { return static_cast<const T*>(a.dres) + row * a.ld_dres; };
+  auto fetch = [&](uint64_t row, GradRow<T, kAligned, kUnits>& g) {
     g.rstd = a.rstd[row];
 #pragma unroll
     for (int j = 0; j < kUnits; ++j) {
       const uint32_t c = (j * kRowThreads + t) * kUnit;
-      g.dy[j] = load_row_unit<T, kAligned>(dy, c, cols, 0.f);
-      if (kAhead && a.dres) g.dres = load_row_unit<T, kAligned>(dres, c, cols, 0.f);
+      g.dy[j] = fetch_unit<T, kAligned>(dy_row(row), row, c, cols, dy_tensor);
+      if (kAhead && a.dres) g.dres = fetch_unit<T, kAligned>(dres_row(row), row, c, cols, dres_tensor);
       g.codes[j] = make_uint2(0u, 0u);
       g.exps[j] = 7u;
       if (c < padded) {
@@ -173,57 +184,57 @@ rmsnorm_grad_kernel(const __grid_constant__ NormGradArgs a, const __grid_constan
       }
     }
   };
-  auto work = [&](uint64_t row, const GradRow<T, kUnits>& g, int turn) {
+  GradRow<T, kAligned, kUnits> g;
+  if (kAhead && first + sub < last) fetch(first + sub, g);
+  int turn = 0;
+  for (uint64_t row = first + sub; row < last; row += kRows, turn ^= 1) {
+    if (!kAhead) fetch(row, g);
+    Unit<T> dy[kUnits], dres;
+    uint2 codes[kUnits];
+    float unit[kUnits];
+    const float rstd = g.rstd;
+#pragma unroll
+    for (int j = 0; j < kUnits; ++j) {
+      const uint32_t c = (j * kRowThreads + t) * kUnit;
+      dy[j] = finish_unit(g.dy[j], dy_row(row), c, cols);
+      if (kAhead && a.dres) dres = finish_unit(g.dres, dres_row(row), c, cols);
+      codes[j] = g.codes[j];
+      unit[j] = act_unit(g.exps[j]);
+    }
+    if (kAhead && row + kRows < last) fetch(row + kRows, g);
     float dot = 0.f;
 #pragma unroll
     for (int j = 0; j < kUnits; ++j) {
       float u[kUnit], n[kUnit], w[kUnit];
-      unit_floats(g.dy[j], u);
-      code_floats(g.codes[j], n);
+      unit_floats(dy[j], u);
+      code_floats(codes[j], n);
       if (!kAhead) weights(j, w);
-      const float unit = act_unit(g.exps[j]);
 #pragma unroll
       for (int k = 0; k < kUnit; ++k) {
-        n[k] *= unit;
-        const float un = u[k] * n[k];
+        const float un = u[k] * (n[k] * unit[j]);
         dw[j][k] += un;
         dot = fmaf(un, kAhead ? kept[k] : w[k], dot);
       }
     }
-    const float mean = row_sum<kRowThreads>(dot, sm[turn]) / static_cast<float>(cols), scale = -mean;
+    const float mean = row_sum<kRowThreads>(dot, sm[turn]) / static_cast<float>(cols);
 #pragma unroll
     for (int j = 0; j < kUnits; ++j) {
       const uint32_t c = (j * kRowThreads + t) * kUnit;
       float u[kUnit], n[kUnit], w[kUnit];
-      unit_floats(g.dy[j], u);
-      code_floats(g.codes[j], n);
+      unit_floats(dy[j], u);
+      code_floats(codes[j], n);
       if (!kAhead) weights(j, w);
-      const float unit = act_unit(g.exps[j]) * scale;
+      const float by = unit[j] * -mean;
 #pragma unroll
-      for (int k = 0; k < kUnit; ++k) u[k] = g.rstd * fmaf(n[k], unit, u[k] * (kAhead ? kept[k] : w[k]));
+      for (int k = 0; k < kUnit; ++k) u[k] = rstd * fmaf(n[k], by, u[k] * (kAhead ? kept[k] : w[k]));
       if (a.dres) {
+        if (!kAhead) dres = finish_unit(fetch_unit<T, kAligned>(dres_row(row), row, c, cols, dres_tensor), dres_row(row), c, cols);
         float r[kUnit];
-        if (kAhead) unit_floats(g.dres, r);
-        else load_values<T, kAligned>(static_cast<const T*>(a.dres) + row * a.ld_dres, c, cols, 0.f, r);
+        unit_floats(dres, r);
 #pragma unroll
         for (int k = 0; k < kUnit; ++k) u[k] += r[k];
       }
       store_row_unit<T, kAligned>(static_cast<T*>(a.dx) + row * a.ld_dx, c, cols, u);
-    }
-  };
-  uint64_t row = first + sub;
-  if (row < last) {
-    GradRow<T, kUnits> one, two;
-    load(row, one);
-    for (;;) {
-      if (kAhead && row + kRows < last) load(row + kRows, two);
-      work(row, one, 0);
-      if ((row += kRows) >= last) break;
-      if (!kAhead) load(row, two);
-      if (kAhead && row + kRows < last) load(row + kRows, one);
-      work(row, two, 1);
-      if ((row += kRows) >= last) break;
-      if (!kAhead) load(row, one);
     }
   }
   if (!a.gw) return;
