@@ -3,28 +3,24 @@
 //   h = x + residual;  rstd = 1 / sqrt(mean(h^2) + eps);  n = h * rstd;  n^ = what the 8-bit codes of n stand for;
 //   y = weight * n^.
 //   u = weight * dy;  dx = dres + rstd * (u - n^ * mean(u * n^));  dweight = sum over the rows of dy * n^.
-// Both are bound by HBM: a row is read once and kept in registers between its sum and its outputs.  kRowThreads
-// threads share a row, a thread owns kUnits units of eight adjacent columns, kRowThreads units apart.
+// Both are bound by HBM: a row is read once and kept in registers between its sum and its outputs.  The threads
+// of a CTA share a row (as many warps as the row has units for), or each of its eight warps has a row of its own
+// (kWarpRow, short rows); a thread owns kUnits units of eight adjacent columns, as many units apart as the row has threads.
 #include "qasg_lm.cuh"
 
 namespace qasg {
 
-// Threads of a CTA: a row's, or eight rows of a warp each.
-template <int kRowThreads> constexpr int kNormThreads = kRowThreads == 32 ? 256 : kRowThreads;
+constexpr int kWarpRows = 8;  // rows of a CTA whose warps have a row each
 
 // Sum over the threads of a row, the same bits in each of them.
-template <int kRowThreads>
+template <bool kWarpRow>
 __device__ __forceinline__ float row_sum(float v, float* sm) {
   v = warp_sum(v);
-  if (kRowThreads == 32) return v;
-  constexpr int kWarps = kRowThreads / 32;
-  if ((threadIdx.x & 31) == 0) sm[threadIdx.x >> 5] = v;
+  if (kWarpRow) return v;
+  const uint32_t lane = threadIdx.x & 31;
+  if (lane == 0) sm[threadIdx.x >> 5] = v;
   __syncthreads();
-  if (kWarps > 8) return warp_sum((threadIdx.x & 31) < kWarps ? sm[threadIdx.x & 31] : 0.f);
-  float s = 0.f;
-#pragma unroll
-  for (int i = 0; i < kWarps; ++i) s += sm[i];
-  return s;
+  return warp_sum(lane < (blockDim.x >> 5) ? sm[lane] : 0.f);
 }
 
 __device__ __forceinline__ void load_weights(const float* __restrict__ weight, uint32_t c, uint32_t cols, float (&w)[kUnit]) {
@@ -37,16 +33,15 @@ __device__ __forceinline__ void load_weights(const float* __restrict__ weight, u
   }
 }
 
-template <typename T, bool kAligned, int kRowThreads, int kUnits>
-__global__ void __launch_bounds__(kNormThreads<kRowThreads>)
+template <typename T, bool kAligned, bool kWarpRow, int kUnits>
+__global__ void __launch_bounds__(kWarpRow ? 32 * kWarpRows : 512)
 rmsnorm_pack_kernel(NormArgs a, ActView act, unsigned int* __restrict__ status) {
-  constexpr int kRows = kNormThreads<kRowThreads> / kRowThreads;
   __shared__ float sm[32];
-  const uint64_t row = static_cast<uint64_t>(blockIdx.x) * kRows + threadIdx.x / kRowThreads;
-  const uint32_t t = threadIdx.x % kRowThreads, cols = act.cols;
+  const uint64_t row = kWarpRow ? static_cast<uint64_t>(blockIdx.x) * kWarpRows + (threadIdx.x >> 5) : blockIdx.x;
+  const uint32_t t = kWarpRow ? threadIdx.x & 31 : threadIdx.x, threads = kWarpRow ? 32 : blockDim.x, cols = act.cols;
   chain_wait();
   chain_trigger();
-  if (kRows > 1 && row >= act.rows) return;  // whole warps: nothing meets below when a row is one warp
+  if (kWarpRow && row >= act.rows) return;  // whole warps: nothing meets below when a row is one warp
   const T* x = static_cast<const T*>(a.x) + row * a.ld_x;
   const T* r = a.residual ? static_cast<const T*>(a.residual) + row * a.ld_r : nullptr;
   Fetched<T, kAligned> fx[kUnits], fr[kUnits];
@@ -54,14 +49,14 @@ rmsnorm_pack_kernel(NormArgs a, ActView act, unsigned int* __restrict__ status) 
   const Extent r_tensor = extent_of(static_cast<const T*>(a.residual), act.rows, a.ld_r, cols);
 #pragma unroll
   for (int j = 0; j < kUnits; ++j) {
-    const uint32_t c = (j * kRowThreads + t) * kUnit;
+    const uint32_t c = (j * threads + t) * kUnit;
     fx[j] = fetch_unit<T, kAligned>(x, row, c, cols, x_tensor);
     if (r) fr[j] = fetch_unit<T, kAligned>(r, row, c, cols, r_tensor);
   }
   float v[kUnits][kUnit];
 #pragma unroll
   for (int j = 0; j < kUnits; ++j) {
-    const uint32_t c = (j * kRowThreads + t) * kUnit;
+    const uint32_t c = (j * threads + t) * kUnit;
     unit_floats(finish_unit(fx[j], x, c, cols), v[j]);
     if (r) {
       float w[kUnit];
@@ -78,15 +73,15 @@ rmsnorm_pack_kernel(NormArgs a, ActView act, unsigned int* __restrict__ status) 
   if (a.h) {
     T* h = static_cast<T*>(a.h) + row * a.ld_h;
 #pragma unroll
-    for (int j = 0; j < kUnits; ++j) store_row_unit<T, kAligned>(h, (j * kRowThreads + t) * kUnit, cols, v[j]);
+    for (int j = 0; j < kUnits; ++j) store_row_unit<T, kAligned>(h, (j * threads + t) * kUnit, cols, v[j]);
   }
-  const float rstd = 1.f / sqrtf(row_sum<kRowThreads>(sq, sm) / static_cast<float>(cols) + a.eps);
+  const float rstd = 1.f / sqrtf(row_sum<kWarpRow>(sq, sm) / static_cast<float>(cols) + a.eps);
   if (t == 0) a.rstd[row] = rstd;
   const uint32_t padded = (cols + kActBlock - 1) & ~static_cast<uint32_t>(kActBlock - 1);
   bool bad = false;
 #pragma unroll
   for (int j = 0; j < kUnits; ++j) {
-    const uint32_t c = (j * kRowThreads + t) * kUnit;
+    const uint32_t c = (j * threads + t) * kUnit;
 #pragma unroll
     for (int k = 0; k < kUnit; ++k) v[j][k] *= rstd;
     const uint32_t b = act_exponent(block_largest(v[j]));
@@ -130,19 +125,15 @@ template <typename T, bool kAligned, int kUnits> struct GradRow {
   float rstd;
 };
 
-// 64 registers, 80 for fp32 where the CTAs are small enough, 128 for the widest rows.
-template <typename T, int kRowThreads, int kUnits>
-constexpr int kGradThreadsPerSm = kUnits > 1 ? kRowThreads : sizeof(T) == 4 && kRowThreads < 512 ? 768 : 1024;
-
-template <typename T, bool kAligned, int kRowThreads, int kUnits>
-__global__ void __launch_bounds__(kNormThreads<kRowThreads>, kGradThreadsPerSm<T, kRowThreads, kUnits> / kNormThreads<kRowThreads>)
+template <typename T, bool kAligned, bool kWarpRow, int kUnits, int kMaxThreads>
+__global__ void __launch_bounds__(kMaxThreads)
 rmsnorm_grad_kernel(const __grid_constant__ NormGradArgs a, const __grid_constant__ ActView act,
                     const __grid_constant__ NormRuns runs) {
-  constexpr int kRows = kNormThreads<kRowThreads> / kRowThreads;
-  constexpr int kCols = kRowThreads * kUnits * kUnit;
+  constexpr int kRows = kWarpRow ? kWarpRows : 1, kCols = 32 * kUnits * kUnit;
   __shared__ float sm[2][32];
-  __shared__ float sm_dw[kRows > 1 ? kRows : 1][kRows > 1 ? kCols : 1];
-  const uint32_t t = threadIdx.x % kRowThreads, cols = act.cols, sub = threadIdx.x / kRowThreads;
+  __shared__ float sm_dw[kRows][kWarpRow ? kCols : 1];
+  const uint32_t t = kWarpRow ? threadIdx.x & 31 : threadIdx.x, threads = kWarpRow ? 32 : blockDim.x, cols = act.cols;
+  const uint32_t sub = kWarpRow ? threadIdx.x >> 5 : 0;
   uint32_t m = 0;
   while (m + 1 < a.M && runs.run0[m + 1] <= blockIdx.x) ++m;
   const uint64_t first = runs.shards.row0[m] + static_cast<uint64_t>(blockIdx.x - runs.run0[m]) * runs.rows_per_run;
@@ -154,7 +145,7 @@ rmsnorm_grad_kernel(const __grid_constant__ NormGradArgs a, const __grid_constan
   float kept[kUnit], dw[kUnits][kUnit];
   auto weights = [&](int j, float (&w)[kUnit]) {
     if (a.weight) {
-      load_weights(a.weight, (j * kRowThreads + t) * kUnit, cols, w);
+      load_weights(a.weight, (j * threads + t) * kUnit, cols, w);
     } else {
 #pragma unroll
       for (int k = 0; k < kUnit; ++k) w[k] = 1.f;
@@ -173,7 +164,7 @@ rmsnorm_grad_kernel(const __grid_constant__ NormGradArgs a, const __grid_constan
     g.rstd = a.rstd[row];
 #pragma unroll
     for (int j = 0; j < kUnits; ++j) {
-      const uint32_t c = (j * kRowThreads + t) * kUnit;
+      const uint32_t c = (j * threads + t) * kUnit;
       g.dy[j] = fetch_unit<T, kAligned>(dy_row(row), row, c, cols, dy_tensor);
       if (kAhead && a.dres) g.dres = fetch_unit<T, kAligned>(dres_row(row), row, c, cols, dres_tensor);
       g.codes[j] = make_uint2(0u, 0u);
@@ -195,7 +186,7 @@ rmsnorm_grad_kernel(const __grid_constant__ NormGradArgs a, const __grid_constan
     const float rstd = g.rstd;
 #pragma unroll
     for (int j = 0; j < kUnits; ++j) {
-      const uint32_t c = (j * kRowThreads + t) * kUnit;
+      const uint32_t c = (j * threads + t) * kUnit;
       dy[j] = finish_unit(g.dy[j], dy_row(row), c, cols);
       if (kAhead && a.dres) dres = finish_unit(g.dres, dres_row(row), c, cols);
       codes[j] = g.codes[j];
@@ -216,10 +207,10 @@ rmsnorm_grad_kernel(const __grid_constant__ NormGradArgs a, const __grid_constan
         dot = fmaf(un, kAhead ? kept[k] : w[k], dot);
       }
     }
-    const float mean = row_sum<kRowThreads>(dot, sm[turn]) / static_cast<float>(cols);
+    const float mean = row_sum<kWarpRow>(dot, sm[turn]) / static_cast<float>(cols);
 #pragma unroll
     for (int j = 0; j < kUnits; ++j) {
-      const uint32_t c = (j * kRowThreads + t) * kUnit;
+      const uint32_t c = (j * threads + t) * kUnit;
       float u[kUnit], n[kUnit], w[kUnit];
       unit_floats(dy[j], u);
       code_floats(codes[j], n);
@@ -239,13 +230,13 @@ rmsnorm_grad_kernel(const __grid_constant__ NormGradArgs a, const __grid_constan
   }
   if (!a.gw) return;
   float* part = a.partials + static_cast<uint64_t>(blockIdx.x) * ((cols + 7u) & ~7u);
-  if (kRows > 1) {
+  if (kWarpRow) {
 #pragma unroll
     for (int j = 0; j < kUnits; ++j)
 #pragma unroll
-      for (int k = 0; k < kUnit; ++k) sm_dw[sub][(j * kRowThreads + t) * kUnit + k] = dw[j][k];
+      for (int k = 0; k < kUnit; ++k) sm_dw[sub][(j * threads + t) * kUnit + k] = dw[j][k];
     __syncthreads();
-    for (uint32_t c = threadIdx.x; c < cols; c += kNormThreads<kRowThreads>) {
+    for (uint32_t c = threadIdx.x; c < cols; c += blockDim.x) {
       float s = 0.f;
 #pragma unroll
       for (int i = 0; i < kRows; ++i) s += sm_dw[i][c];
@@ -254,7 +245,7 @@ rmsnorm_grad_kernel(const __grid_constant__ NormGradArgs a, const __grid_constan
   } else {
 #pragma unroll
     for (int j = 0; j < kUnits; ++j) {
-      const uint32_t c = (j * kRowThreads + t) * kUnit;
+      const uint32_t c = (j * threads + t) * kUnit;
       if (c < cols) store_unit(part + c, pack_unit<float>(dw[j]));  // rows of partials are whole units
     }
   }
@@ -285,25 +276,8 @@ run_sum_kernel(const float* __restrict__ partials, const __grid_constant__ NormR
 }
 
 // ------------------------------------------------------------------ launchers
-template <typename F> static void with_row(uint32_t cols, F f) {
-  using std::integral_constant;
-  if (cols <= 256) f(integral_constant<int, 32>(), integral_constant<int, 1>());
-  else if (cols <= 1024) f(integral_constant<int, 32>(), integral_constant<int, 4>());
-  else if (cols <= 2048) f(integral_constant<int, 128>(), integral_constant<int, 2>());
-  else if (cols <= 4096) f(integral_constant<int, 256>(), integral_constant<int, 2>());
-  else if (cols <= 8192) f(integral_constant<int, 512>(), integral_constant<int, 2>());
-  else f(integral_constant<int, 512>(), integral_constant<int, 4>());  // up to kNormMaxCols
-}
-// The gradient keeps a column's sum and weight beside two rows: one unit a thread.
-template <typename F> static void with_grad_row(uint32_t cols, F f) {
-  using std::integral_constant;
-  if (cols <= 256) f(integral_constant<int, 32>(), integral_constant<int, 1>());
-  else if (cols <= 1024) f(integral_constant<int, 128>(), integral_constant<int, 1>());
-  else if (cols <= 2048) f(integral_constant<int, 256>(), integral_constant<int, 1>());
-  else if (cols <= 4096) f(integral_constant<int, 512>(), integral_constant<int, 1>());
-  else if (cols <= 8192) f(integral_constant<int, 1024>(), integral_constant<int, 1>());
-  else f(integral_constant<int, 512>(), integral_constant<int, 4>());  // up to kNormMaxCols
-}
+// Threads for a row of `cols` columns with `units` units each.
+static unsigned row_threads(uint32_t cols, uint32_t units) { return (cols + 32 * kUnit * units - 1) / (32 * kUnit * units) * 32; }
 
 int launch_rmsnorm_pack(int dtype, const NormArgs& a, const ActView& act, unsigned int* status, const LaunchShape& shape,
                         cudaStream_t stream) {
@@ -311,22 +285,24 @@ int launch_rmsnorm_pack(int dtype, const NormArgs& a, const ActView& act, unsign
                    (!a.h || rows_aligned(dtype, a.h, a.ld_h)) && (!a.y || rows_aligned(dtype, a.y, a.ld_y));
   with_dtype_aligned(dtype, all, [&](auto t, auto aligned) {
     using T = decltype(t);
-    with_row(act.cols, [&](auto row_threads, auto units) {
-      constexpr int kThreadsRow = decltype(row_threads)::value;
-      constexpr unsigned kRows = kNormThreads<kThreadsRow> / kThreadsRow;
-      launch_lm(rmsnorm_pack_kernel<T, decltype(aligned)::value, kThreadsRow, decltype(units)::value>,
-                dim3(static_cast<unsigned>((act.rows + kRows - 1) / kRows)), kNormThreads<kThreadsRow>, 0, 1, stream,
-                shape.chained, a, act, status);
-    });
+    auto go = [&](auto kernel, unsigned rows, unsigned threads) {
+      launch_lm(kernel, dim3(static_cast<unsigned>((act.rows + rows - 1) / rows)), threads, 0, 1, stream, shape.chained, a, act, status);
+    };
+    constexpr bool kAll = decltype(aligned)::value;
+    if (act.cols <= 32 * kUnit) go(rmsnorm_pack_kernel<T, kAll, true, 1>, kWarpRows, 32 * kWarpRows);
+    else if (act.cols <= 4 * 32 * kUnit) go(rmsnorm_pack_kernel<T, kAll, true, 4>, kWarpRows, 32 * kWarpRows);
+    else if (act.cols <= 2 * 512 * kUnit) go(rmsnorm_pack_kernel<T, kAll, false, 2>, 1, row_threads(act.cols, 2));
+    else go(rmsnorm_pack_kernel<T, kAll, false, 4>, 1, row_threads(act.cols, 4));  // up to kNormMaxCols
   });
   return 1;
 }
 
-// Runs of rows: about one for each CTA that 148 SMs hold, plus what the workers' ends add.
+// The gradient keeps a column's sum and weight beside two rows: one unit a thread, four for the widest rows.
+constexpr uint32_t kGradWide = 1024 * kUnit;
+// Runs of rows: about one for each CTA that 148 SMs hold at 64 registers, plus what the workers' ends add.
 static uint32_t norm_runs(uint32_t cols) {
-  uint32_t runs = 0;
-  with_grad_row(cols, [&](auto row_threads, auto) { runs = 148u * (1024u / kNormThreads<decltype(row_threads)::value>); });
-  return runs;
+  const unsigned threads = cols <= 32 * kUnit ? 32 * kWarpRows : row_threads(cols, cols > kGradWide ? 4 : 1);
+  return 148u * (1024u / threads);
 }
 uint64_t rmsnorm_grad_scratch_bytes(uint64_t cols, uint32_t M) {
   return (norm_runs(static_cast<uint32_t>(cols)) + M) * ((cols + 7) & ~7ull) * sizeof(float);
@@ -353,11 +329,11 @@ int launch_rmsnorm_grad(int dtype, const NormGradArgs& a, const ActView& act, co
                      rows_aligned(dtype, a.dx, a.ld_dx);
     with_dtype_aligned(dtype, all, [&](auto t, auto aligned) {
       using T = decltype(t);
-      with_grad_row(act.cols, [&](auto row_threads, auto units) {
-        constexpr int kThreadsRow = decltype(row_threads)::value;
-        launch_lm(rmsnorm_grad_kernel<T, decltype(aligned)::value, kThreadsRow, decltype(units)::value>, dim3(runs.run0[a.M]),
-                  kNormThreads<kThreadsRow>, 0, 1, stream, shape.chained, a, act, runs);
-      });
+      auto go = [&](auto kernel, unsigned threads) { launch_lm(kernel, dim3(runs.run0[a.M]), threads, 0, 1, stream, shape.chained, a, act, runs); };
+      constexpr bool kAll = decltype(aligned)::value;
+      if (act.cols <= 32 * kUnit) go(rmsnorm_grad_kernel<T, kAll, true, 1, 32 * kWarpRows>, 32 * kWarpRows);
+      else if (act.cols <= kGradWide) go(rmsnorm_grad_kernel<T, kAll, false, 1, 1024>, row_threads(act.cols, 1));
+      else go(rmsnorm_grad_kernel<T, kAll, false, 4, 512>, row_threads(act.cols, 4));  // up to kNormMaxCols
     });
     ++launches;
   }
