@@ -1,0 +1,109 @@
+"""Trains the last block of a small language model with quantized adaptive subgradient steps.
+
+M workers hold different tokens of a synthetic text (the next token is a fixed function of the current one, with noise).
+Every step runs, for all workers at once,
+  norm of the residual stream, its output kept in 8 bits   (rmsnorm_pack)
+  logits = y W^T                                           (torch)
+  log probabilities of the next tokens, entropy            (token_logprob)
+  their gradient, written over the logits                  (token_logprob_grad)
+  each worker's gradient of W, from the 8 bits             (act_wgrad)
+  each worker's gradient of the norm's weight              (rmsnorm_grad)
+into the workers' gradient rows g [M][W | norm weight], and the parameters x take one quantized step (step).
+
+The rule is composite mirror descent: dual averaging measures its steps from 0, where a norm's weight silences its layer.
+
+  python examples/lm_head_training.py [--steps 60]
+"""
+import argparse
+import os
+import sys
+
+import torch
+
+sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+from paper_2208_05631_b200 import libqasg  # noqa: E402
+
+EPS = 1e-5
+
+
+class LmHead:
+    """The parameters, buffers and handles of the training loop."""
+
+    def __init__(self, workers=4, tokens_per_worker=256, dim=256, vocab=1000, seed=0, device="cuda"):
+        self.M, self.rows, self.dim, self.vocab = workers, workers * tokens_per_worker, dim, vocab
+        gen = torch.Generator(device=device).manual_seed(seed)
+        rand = lambda *shape: torch.randn(shape, generator=gen, device=device)  # noqa: E731
+        self.gen, self.device = gen, device
+        self.embedding = rand(vocab, dim).to(torch.bfloat16)       # the residual stream below: not trained
+        self.branch = (0.3 * rand(vocab, dim)).to(torch.bfloat16)  # what the block before adds to it
+        self.successor = torch.randint(0, vocab, (vocab,), generator=gen, device=device)
+        self.nw = vocab * dim
+        self.d = self.nw + dim                       # parameters: W, then the norm's weight
+        self.ld = (self.d + 3) // 4 * 4
+        self.x = torch.zeros(self.d, device=device)
+        self.x[: self.nw] = 0.02 * rand(self.nw)
+        self.x[self.nw:] = 1.0
+        self.h = torch.zeros(self.d, device=device)
+        self.g = torch.zeros((workers, self.ld), device=device)
+        bf16 = lambda *shape: torch.empty(shape, dtype=torch.bfloat16, device=device)  # noqa: E731
+        f32 = lambda *shape: torch.empty(shape, device=device)  # noqa: E731
+        self.y, self.dx, self.stream = bf16(self.rows, dim), bf16(self.rows, dim), bf16(self.rows, dim)
+        self.rstd, self.logprob, self.entropy, self.lse = (f32(self.rows) for _ in range(4))
+        self.act = libqasg.new_act(self.rows, dim, device)
+        self.shards = [m * tokens_per_worker for m in range(workers + 1)]
+        self.scratch = libqasg.new_scratch(max(libqasg.act_wgrad_scratch_bytes(vocab, dim, workers),
+                                               libqasg.rmsnorm_grad_scratch_bytes(dim, workers)), device)
+        # the loss of a worker is the mean over its own tokens: one factor for every token
+        self.g_logprob = torch.full((self.rows,), -1.0 / tokens_per_worker, device=device)
+        self.ctx = libqasg.Context(self.d, workers, device=torch.cuda.current_device())
+
+    def batch(self):
+        now = torch.randint(0, self.vocab, (self.rows,), generator=self.gen, device=self.device)
+        noise = torch.rand((self.rows,), generator=self.gen, device=self.device) < 0.05
+        other = torch.randint(0, self.vocab, (self.rows,), generator=self.gen, device=self.device)
+        return now, torch.where(noise, other, self.successor[now])
+
+    def gradients(self, now, then):
+        """Fills g with the workers' gradients; returns the mean loss and entropy (device scalars)."""
+        ctx, B, dim, V, rows = self.ctx, libqasg.BF16, self.dim, self.vocab, self.rows
+        W, norm_weight = self.x[: self.nw].view(V, dim).to(torch.bfloat16), self.x[self.nw:]
+        below, branch = self.embedding[now], self.branch[now]
+        ctx.rmsnorm_pack(B, below, dim, branch, dim, norm_weight, EPS, self.stream, dim, self.y, dim, self.act, self.rstd)
+        logits = self.y @ W.t()
+        ctx.token_logprob(B, logits, V, rows, V, then, self.logprob, self.entropy, self.lse)
+        ctx.token_logprob_grad(B, logits, V, rows, V, then, self.lse, None, self.g_logprob, None, None, logits, V)
+        # y = norm weight * n^ and act holds n^: the weight's factor goes into the product's columns
+        ctx.act_wgrad(B, logits, V, V, self.act, norm_weight, self.M, self.shards, self.g, self.ld, dim, False, self.scratch)
+        ctx.rmsnorm_grad(B, logits @ W, dim, None, 0, self.act, self.rstd, norm_weight, self.M, self.shards, self.dx, dim,
+                         self.g[:, self.nw:], self.ld, False, self.scratch)
+        return -self.logprob.mean(), self.entropy.mean()
+
+    def step(self, t, params):
+        self.ctx.step(libqasg.RULE_CMD, self.g, self.d, self.ld, self.M, t, params, self.x, self.h)
+
+
+def train(steps=60, report=None, **sizes):
+    """Runs the loop; returns the model and the loss of every step."""
+    model = LmHead(**sizes)
+    params = libqasg.make_params(lam=1e-7, eta=0.02, delta=1e-8)
+    losses = []
+    for t in range(1, steps + 1):
+        loss, entropy = model.gradients(*model.batch())
+        model.step(t, params)
+        losses.append(loss)
+        if report and (t == 1 or t % report == 0):
+            print("step %4d  loss %.4f  entropy %.4f" % (t, float(loss), float(entropy)))
+    status = model.ctx.last_async_status()
+    if status != libqasg.OK:
+        raise libqasg.QasgError(status, "lm_head_training")
+    return model, [float(v) for v in losses]
+
+
+def main():
+    ap = argparse.ArgumentParser(description=__doc__.splitlines()[0])
+    ap.add_argument("--steps", type=int, default=60)
+    train(ap.parse_args().steps, report=10)
+
+
+if __name__ == "__main__":
+    main()
