@@ -139,10 +139,19 @@ __device__ __forceinline__ Fetched<T, kAligned> fetch_unit(const T* row, uint64_
   }
   return f;
 }
+// Zeros from column n on in the unit at column c.
+template <typename T> __device__ __forceinline__ void clear_past(Unit<T>& u, uint32_t c, uint32_t n) {
+  constexpr int kEach = 4 / sizeof(T);
+#pragma unroll
+  for (int i = 0; i < static_cast<int>(sizeof(u) / 4); ++i) {
+    if (c + i * kEach >= n) u.w[i] = 0u;
+    else if (kEach == 2 && c + i * kEach + 1 >= n) u.w[i] &= 0xffffu;
+  }
+}
 // Zeros past the end of the row.
 template <typename T, bool kAligned>
 __device__ __forceinline__ Unit<T> finish_unit(const Fetched<T, kAligned>& f, const T* row, uint32_t c, uint32_t n) {
-  constexpr int kWords = sizeof(Unit<T>) / 4, kEach = 4 / sizeof(T);
+  constexpr int kWords = sizeof(Unit<T>) / 4;
   Unit<T> u;
   if constexpr (kAligned) {
 #pragma unroll
@@ -150,13 +159,7 @@ __device__ __forceinline__ Unit<T> finish_unit(const Fetched<T, kAligned>& f, co
   } else {
     shifted_words<kWords>(f.w, static_cast<uint32_t>(reinterpret_cast<uintptr_t>(row)) & 15u, u.w);
   }
-  if (c + kUnit > n) {
-#pragma unroll
-    for (int i = 0; i < kWords; ++i) {
-      if (c + i * kEach >= n) u.w[i] = 0u;
-      else if (kEach == 2 && c + i * kEach + 1 >= n) u.w[i] &= 0xffffu;
-    }
-  }
+  if (c + kUnit > n) clear_past(u, c, n);
   return u;
 }
 

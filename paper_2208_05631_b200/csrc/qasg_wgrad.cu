@@ -49,15 +49,22 @@ constexpr int kTurnCols = 16, kTurnPitch = 20;  // floats: rows of whole 16-byte
 constexpr long long kMaxWait = 1ll << 34;                  // bound of every wait in cycles (some seconds)
 
 // How dy reaches shared memory, as 1, 2 or 3 bf16 pieces: 16-bit rows on 16-byte boundaries by TMA (fp16 is then split
-// in place by the converting warps), everything else through those warps' registers.
+// in place by the converting warps); everything else in the aligned words around each row (cp.async), which four of the
+// converting warps shift and split.
 template <typename T> constexpr int kPieces = 1;
 template <> constexpr int kPieces<__half> = 2;
 template <> constexpr int kPieces<float> = 3;
-// Stages of the two rings: operands (the pieces of dy, then the converted codes), and codes as they come.
-template <int kP> constexpr int kStages = kP == 1 ? 5 : kP == 2 ? 3 : 2;
-constexpr int kCodeStages = 4;
+// Stages of the two rings: operands (the pieces of dy, then the converted codes), and codes as they come; and, where
+// dy does not come by TMA, the halves of a stage (32 rows, in the aligned words around them) that are on their way.
+template <int kP, bool kTma> constexpr int kStages = kTma ? (kP == 1 ? 5 : 3) : kP == 1 ? 3 : 2;
+template <int kP> constexpr int kCodeStages = kP == 3 ? 3 : 4;
+template <int kP, bool kTma> constexpr int kHalves = kTma ? 0 : kP == 3 ? 3 : 8;
+constexpr int kHalfRows = kWgRows / 2;
+template <typename T> constexpr uint32_t kRawPitch = kWgHalf * sizeof(T) + 16;
 template <int kP> constexpr uint32_t kStageBytes = (kP + 1) * kOperandBytes;
-template <int kP> constexpr uint32_t kWgSmem = kStages<kP> * kStageBytes<kP> + kCodeStages * kCodeStage + 8 * 32 * kTurnPitch * 4 + 1024;
+template <typename T, bool kTma>
+constexpr uint32_t kWgSmem = kStages<kPieces<T>, kTma> * kStageBytes<kPieces<T>> + kCodeStages<kPieces<T>> * kCodeStage +
+                             kHalves<kPieces<T>, kTma> * kHalfRows * kRawPitch<T> + 8 * 32 * kTurnPitch * 4 + 1024;
 
 struct WgradPlan {
   uint32_t row0[kMaxWorkers + 1];
@@ -197,7 +204,7 @@ __device__ __forceinline__ TileWork unit_of(const WgradPlan& p, uint32_t u) {
   r.k0 = across * kWgTile;
   const uint32_t first = p.row0[r.worker], end = p.row0[r.worker + 1];
   r.row0 = first, r.row1 = end, r.slot = -1;
-  if (pieces > 1) {  // whole stages; at most 2^25 of them times kMaxPairs
+  if (pieces > 1) {  // whole stages; at most 2^25 of them, cut in less than 2^7
     const uint32_t steps = (end - first + kWgRows - 1) / kWgRows;
     r.row0 = min(first + steps * piece / pieces * kWgRows, end);
     r.row1 = min(first + steps * (piece + 1) / pieces * kWgRows, end);
@@ -298,36 +305,134 @@ __device__ __forceinline__ uint4 leading_bits(float (&v)[kUnit]) {
   uint32_t q[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) q[j] = __byte_perm(__float_as_uint(v[2 * j]), __float_as_uint(v[2 * j + 1]), 0x7632);
-  float largest = fabsf(v[0]);
-#pragma unroll
-  for (int j = 1; j < kUnit; ++j) largest = max_nan(largest, fabsf(v[j]));
-  const bool finite = largest < INFINITY;
+  float most = 0.f, rest[kUnit];
 #pragma unroll
   for (int j = 0; j < kUnit; ++j) {
-    const float rest = v[j] - __uint_as_float(__float_as_uint(v[j]) & 0xffff0000u);
-    v[j] = finite || fabsf(v[j]) < INFINITY ? rest : 0.f;
+    most = fmaxf(most, fabsf(v[j]));
+    rest[j] = v[j] - __uint_as_float(__float_as_uint(v[j]) & 0xffff0000u);
   }
+  if (most == INFINITY) {
+#pragma unroll
+    for (int j = 0; j < kUnit; ++j) rest[j] = fabsf(v[j]) == INFINITY ? 0.f : rest[j];
+  }
+#pragma unroll
+  for (int j = 0; j < kUnit; ++j) v[j] = rest[j];
   return make_uint4(q[0], q[1], q[2], q[3]);
 }
 
-// The raw words of columns [c, c + 8) of a row of n values, zeros past its end; any alignment.
-template <typename T> __device__ __forceinline__ Unit<T> load_raw(const T* row, uint32_t c, uint32_t n) {
-  if (c + kUnit <= n && is_aligned16(row + c)) return load_unit(row + c);
-  Unit<T> u;
-#pragma unroll
-  for (int i = 0; i < static_cast<int>(sizeof(u) / 4); ++i) {
-    constexpr int kEach = 4 / sizeof(T);
-    u.w[i] = 0u;
-#pragma unroll
-    for (int j = 0; j < kEach; ++j)
-      if (c + i * kEach + j < n) {
-        const T v = row[c + i * kEach + j];
-        if (sizeof(T) == 2) u.w[i] |= static_cast<uint32_t>(*reinterpret_cast<const uint16_t*>(&v)) << (16 * j);
-        else u.w[i] = *reinterpret_cast<const uint32_t*>(&v);
-      }
+// The halves of stages, in the order in which a pair works on them.
+struct HalfStage {
+  uint32_t u, row, end, n0, half;  // unit; first row of the half, end of the unit's rows; first column; 0 or 1
+};
+__device__ __forceinline__ void enter_unit(HalfStage& h, const WgradPlan& plan, uint32_t pairs) {
+  for (; h.u < plan.units; h.u += pairs) {  // the next unit that has rows
+    const TileWork w = unit_of(plan, h.u);
+    h.row = w.row0, h.end = w.row1, h.n0 = w.n0, h.half = 0;
+    if (w.row0 < w.row1) return;
   }
-  return u;
 }
+__device__ __forceinline__ HalfStage first_half(const WgradPlan& plan, uint32_t pair, uint32_t pairs) {
+  HalfStage h = {pair, 0, 0, 0, 0};
+  enter_unit(h, plan, pairs);
+  return h;
+}
+__device__ __forceinline__ void next_half(HalfStage& h, const WgradPlan& plan, uint32_t pairs) {
+  h.row += kHalfRows;
+  h.half ^= 1u;
+  if (h.half == 0 && h.row >= h.end) {
+    h.u += pairs;
+    enter_unit(h, plan, pairs);
+  }
+}
+// Meeting of the group of four warps that brings dy; true if all of them say so.
+__device__ __forceinline__ bool group_agrees(bool ok) {
+  uint32_t all;
+  asm volatile(
+      "{\n.reg .pred p, q;\nsetp.ne.u32 q, %1, 0;\nbar.red.and.pred p, 1, %2, q;\nselp.u32 %0, 1, 0, p;\n}"
+      : "=r"(all) : "r"(static_cast<uint32_t>(ok)), "n"(kGroupWarps * 32) : "memory");
+  return all != 0;
+}
+
+// Rows of dy on any boundary, 128 columns from n0 + first on.
+template <typename T> struct DyRows {
+  static constexpr uint32_t kVectors = kRawPitch<T> / 16;  // of 16 bytes around a row's 128 columns
+  const T* dy;
+  uint64_t ld, rows;
+  uint32_t n, first;
+
+  __device__ __forceinline__ const T* at(const HalfStage& h, uint32_t row) const {
+    return dy + static_cast<uint64_t>(h.row + row) * ld + h.n0 + first;
+  }
+  // Asks for a half's words, those that lie in the tensor and hold a column of it: four threads a row.
+  __device__ __forceinline__ void fetch(const HalfStage& h, uint32_t to, uint32_t ctid) const {
+    const uint32_t row = ctid >> 2, part = ctid & 3u;
+    if (h.row + row >= h.end || h.n0 + first >= n) return;
+    const char* lo = reinterpret_cast<const char*>(dy);
+    const char* hi = reinterpret_cast<const char*>(dy + (rows - 1) * ld + n);
+    const T* begin = at(h, row);
+    const char* end = reinterpret_cast<const char*>(begin + (n - h.n0 - first));  // of the row's columns
+    const char* from = reinterpret_cast<const char*>(reinterpret_cast<uintptr_t>(begin) & ~static_cast<uintptr_t>(15)) + part * 16;
+    uint32_t dst = to + row * kRawPitch<T> + part * 16;
+    if (from - part * 16 >= lo && from - part * 16 + kVectors * 16 <= end) {
+#pragma unroll
+      for (uint32_t v = 0; v + 1 < kVectors; v += 4)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + v * 16), "l"(from + v * 16) : "memory");
+      if (part == 0)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + (kVectors - 1) * 16), "l"(from + (kVectors - 1) * 16) : "memory");
+      return;
+    }
+#pragma unroll 1
+    for (uint32_t v = part; v < kVectors && from < end; v += 4, from += 64, dst += 64) {
+      if (from >= lo) {
+        const uint32_t bytes = hi - from < 16 ? static_cast<uint32_t>(hi - from) : 16u;
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(from), "r"(bytes) : "memory");
+      } else {  // the words the tensor begins in
+        uint32_t w[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int b = 0; b < 16; b += sizeof(T)) {
+          if (from + b < lo || from + b >= hi) continue;
+          if (sizeof(T) == 4) w[b / 4] = *reinterpret_cast<const uint32_t*>(from + b);
+          else w[b / 4] |= static_cast<uint32_t>(*reinterpret_cast<const uint16_t*>(from + b)) << (8 * (b & 2));
+        }
+        store_shared(dst, make_uint4(w[0], w[1], w[2], w[3]));
+      }
+    }
+  }
+  // Shifts and splits a half that has landed: a thread takes a chunk of eight columns of rows r, r + 8, ...
+  __device__ __forceinline__ void finish(const HalfStage& h, uint32_t raw, uint32_t to, uint32_t ctid) const {
+    constexpr int kWords = sizeof(Unit<T>) / 4;
+    const uint32_t chunk = ctid & 15u, c = h.n0 + first + chunk * kUnit, r0 = ctid >> 4;
+    const uint32_t pitch = static_cast<uint32_t>(ld * sizeof(T));  // the low bits decide a row's shift
+    uint32_t shift = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(at(h, r0)));
+    uint32_t from = raw + r0 * kRawPitch<T> + chunk * (kUnit * sizeof(T)), out = to + chunk_offset(h.half * kHalfRows + r0, chunk);
+    const uint32_t valid = c < n && h.row + r0 < h.end ? h.end - h.row - r0 : 0u;  // rows from r0 on
+#pragma unroll
+    for (uint32_t i = 0; i < kHalfRows / 8; ++i) {
+      uint32_t x[kWords + 4];
+      Unit<T> u;
+#pragma unroll
+      for (int k = 0; k < kWords / 4 + 1; ++k) {
+        const uint4 v = load_shared(from + i * 8 * kRawPitch<T> + k * 16);
+        x[4 * k] = v.x, x[4 * k + 1] = v.y, x[4 * k + 2] = v.z, x[4 * k + 3] = v.w;
+      }
+      shifted_words<kWords>(x, (shift + i * 8 * pitch) & 15u, u.w);
+      if (8 * i >= valid) {
+#pragma unroll
+        for (int k = 0; k < kWords; ++k) u.w[k] = 0u;
+      } else if (c + kUnit > n) {
+        clear_past(u, c, n);
+      }
+      if constexpr (kPieces<T> == 1) {
+        store_shared(out + i * 1024, make_uint4(u.w[0], u.w[1], u.w[2], u.w[3]));
+      } else {
+        float v[kUnit];
+        unit_floats(u, v);
+#pragma unroll
+        for (int p = 0; p < kPieces<T>; ++p) store_shared(out + p * kOperandBytes + i * 1024, leading_bits(v));
+      }
+    }
+  }
+};
 
 // ------------------------------------------------------------------ kernel
 template <typename T, bool kTma>
@@ -335,30 +440,30 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWgThreads, 1)
 act_wgrad_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_constant__ CUtensorMap map_codes,
                  const __grid_constant__ CUtensorMap map_exps, const __grid_constant__ WgradPlan plan,
                  const __grid_constant__ WgradArgs a, uint32_t cols, unsigned int* __restrict__ status) {
-  constexpr int kP = kPieces<T>, kN = kStages<kP>;
+  constexpr int kP = kPieces<T>, kN = kStages<kP, kTma>, kC = kCodeStages<kP>, kRaw = kHalves<kP, kTma>;
   constexpr uint32_t kStage = kStageBytes<kP>;
   constexpr int kSegment = kSegmentSteps / (kWgRows / 16) / kP;  // stages of a segment
   extern __shared__ uint8_t smem_raw[];
-  __shared__ __align__(8) uint64_t bars[3 * kN + 2 * kCodeStages + 4];
+  __shared__ __align__(8) uint64_t bars[3 * kN + 2 * kC + 4];
   __shared__ uint32_t tmem_base, gave_up, last_at, last_phase;
   const uint32_t tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   uint32_t rank;
   asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
   const uint32_t pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
   const uint32_t at_ring = (smem_addr(smem_raw) + 1023u) & ~1023u, at_codes = at_ring + kN * kStage,
-                 at_turn = at_codes + kCodeStages * kCodeStage;
+                 at_turn = at_codes + kC * kCodeStage, at_raw = at_turn + 8 * 32 * kTurnPitch * 4;
   // full: a copy has landed in this CTA (of dy, of codes); ready: both CTAs' part of a stage can be multiplied (the
   // first CTA's barriers count); empty: a stage may be overwritten
   const uint32_t full = smem_addr(bars), ready = full + 8 * kN, empty = ready + 8 * kN, code_full = empty + 8 * kN,
-                 code_empty = code_full + 8 * kCodeStages, acc_full = code_empty + 8 * kCodeStages, acc_empty = acc_full + 16;
+                 code_empty = code_full + 8 * kC, acc_full = code_empty + 8 * kC, acc_empty = acc_full + 16;
   if (tid == 0) {
     gave_up = 0u;
     for (int s = 0; s < kN; ++s) {
       barrier_init(full + 8 * s, 1);
-      barrier_init(ready + 8 * s, 2 * kGroupWarps + (kTma && kP == 1 ? 2 : 0));
+      barrier_init(ready + 8 * s, 2 * kGroupWarps + (!kTma ? 2 * kGroupWarps : kP == 1 ? 2 : 0));
       barrier_init(empty + 8 * s, 1);
     }
-    for (int s = 0; s < kCodeStages; ++s) {
+    for (int s = 0; s < kC; ++s) {
       barrier_init(code_full + 8 * s, 1);
       barrier_init(code_empty + 8 * s, kGroupWarps);
     }
@@ -391,7 +496,7 @@ act_wgrad_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_consta
       // copies
       const bool one = elect_one();
       Ring<kN> r = {0, 0};
-      Ring<kCodeStages> rc = {0, 0};
+      Ring<kC> rc = {0, 0};
       uint32_t issued = 0;
       bool ok = true;
       for (uint32_t u = pair; u < plan.units && ok; u += pairs) {
@@ -420,7 +525,7 @@ act_wgrad_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_consta
         }
       }
       if (!ok) {  // gave up: the copies in flight land before the CTA leaves
-        for (uint32_t i = min(issued + 1, static_cast<uint32_t>(kCodeStages)); i > 0; --i) {
+        for (uint32_t i = min(issued + 1, static_cast<uint32_t>(kC)); i > 0; --i) {
           rc.back();
           barrier_drain(code_full + 8 * rc.at, rc.phase);
         }
@@ -491,11 +596,9 @@ act_wgrad_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_consta
       }
     }
   } else if (warp >= kFirstConvert) {
-    // conversion: the groups of warps take stages in turn; a thread takes 16 columns (seg) of rows r, r + 16, ...
+    // conversion: by TMA the groups of warps take stages in turn, otherwise one brings dy and the other converts codes
     fewer_registers<kConvertRegs>();
-    constexpr int kLoads = sizeof(T) == 4 ? 2 : 4;  // chunks of dy a thread has in flight
     const uint32_t group = (warp - kFirstConvert) / kGroupWarps, ctid = tid - (kFirstConvert + group * kGroupWarps) * 32;
-    const uint32_t chunk = ctid & 15u;
     // a thread takes eight columns (seg) of either atom in rows r0, r0 + 16, ...; threads of odd rows take the
     // second atom first, so that 16 threads' loads cover all banks
     const uint32_t seg = ctid & 7u, r0 = ctid >> 3, second = r0 & 1u;
@@ -505,25 +608,46 @@ act_wgrad_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_consta
     const T* dy = static_cast<const T*>(a.dy);
     const uint32_t ready_of_first = map_rank(ready, 0), code_empty_own = map_rank(code_empty, rank);
     Ring<kN> r = {0, 0};
-    Ring<kCodeStages> rc = {0, 0};
+    if constexpr (!kTma) {
+      if (group == 1) {  // dy
+        const DyRows<T> from = {dy, a.ld_dy, a.rows, a.out_cols, rank * kWgHalf};
+        HalfStage ahead = first_half(plan, pair, pairs), now = ahead;
+        auto fetch = [&](uint32_t buffer) {
+          if (ahead.u < plan.units) {
+            from.fetch(ahead, at_raw + buffer * kHalfRows * kRawPitch<T>, ctid);
+            next_half(ahead, plan, pairs);
+          }
+          asm volatile("cp.async.commit_group;" ::: "memory");
+        };
+        for (uint32_t i = 0; i + 1 < kRaw; ++i) fetch(i);
+        bool ok = true;
+        for (uint32_t buffer = 0; now.u < plan.units; buffer = buffer + 1 == kRaw ? 0 : buffer + 1) {
+          asm volatile("cp.async.wait_group %0;" ::"n"(kRaw - 2) : "memory");
+          // every warp's words of this half have landed, and everybody is done with the half before: its place is free
+          if (!(ok = group_agrees(ok))) break;
+          fetch(buffer == 0 ? kRaw - 1 : buffer - 1);
+          if (now.half == 0) ok = all_wait(empty + 8 * r.at, r.phase ^ 1u, &gave_up);
+          if (ok) from.finish(now, at_raw + buffer * kHalfRows * kRawPitch<T>, at_ring + r.at * kStage, ctid);
+          if (now.half == 1) {
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (ok && lane == 0) barrier_arrive_cluster(ready_of_first + 8 * r.at);
+            r.next();
+          }
+          next_half(now, plan, pairs);
+        }
+        asm volatile("cp.async.wait_all;" ::: "memory");
+      }
+    }
+    Ring<kC> rc = {0, 0};
     uint32_t turn = 0;
     bool ok = true;
-    for (uint32_t u = pair; u < plan.units && ok; u += pairs) {
+    for (uint32_t u = pair; u < plan.units && ok && (kTma || group == 0); u += pairs) {
       const TileWork w = unit_of(plan, u);
       const uint32_t exp_at = ((w.k0 + rank * kWgHalf) / kActBlock) & 15u;  // four blocks: one word
-      const uint32_t n = w.n0 + rank * kWgHalf + chunk * kUnit;
       for (uint32_t t = w.row0; t < w.row1; t += kWgRows, r.next(), rc.next(), turn ^= 1u) {
-        if (turn != group) continue;
+        if (kTma && turn != group) continue;
         const uint32_t rows = min(static_cast<uint32_t>(kWgRows), w.row1 - t);
-        Unit<T> raw[kTma ? 1 : kLoads];
-        auto load = [&](int batch) {
-#pragma unroll
-          for (int i = 0; i < kLoads; ++i) {
-            const uint32_t y = (ctid >> 4) + 8 * (batch * kLoads + i);
-            raw[kTma ? 0 : i] = load_raw<T>(dy + static_cast<uint64_t>(t + y) * a.ld_dy, n, y < rows ? a.out_cols : 0u);
-          }
-        };
-        if (!kTma) load(0);
         if (!(ok = all_wait(code_full + 8 * rc.at, rc.phase, &gave_up))) break;
         if (!(ok = all_wait(empty + 8 * r.at, r.phase ^ 1u, &gave_up))) break;
         const uint32_t codes = at_codes + rc.at * kCodeStage, stage = at_ring + r.at * kStage, out = stage + kP * kOperandBytes;
@@ -553,7 +677,7 @@ act_wgrad_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_consta
           if (!(ok = all_wait(full + 8 * r.at, r.phase, &gave_up))) break;
 #pragma unroll 2
           for (int i = 0; i < 8; ++i) {
-            const uint32_t y = (ctid >> 4) + 8 * i, at = stage + chunk_offset(y, chunk);
+            const uint32_t y = (ctid >> 4) + 8 * i, at = stage + chunk_offset(y, ctid & 15u);
             uint4 q = load_shared(at);
             if (y >= rows) q = make_uint4(0u, 0u, 0u, 0u);  // rows of another worker came with the copy
             Unit<T> u;
@@ -562,19 +686,6 @@ act_wgrad_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_consta
             unit_floats(u, v);
             store_shared(at, leading_bits(v));
             store_shared(at + kOperandBytes, leading_bits(v));
-          }
-        }
-        if (!kTma) {
-          for (int batch = 0; batch < 8 / kLoads; ++batch) {
-            if (batch) load(batch);
-#pragma unroll
-            for (int i = 0; i < (kTma ? 1 : kLoads); ++i) {
-              float v[kUnit];
-              unit_floats(raw[i], v);
-#pragma unroll
-              for (int p = 0; p < kP; ++p)
-                store_shared(stage + p * kOperandBytes + chunk_offset((ctid >> 4) + 8 * (batch * kLoads + i), chunk), leading_bits(v));
-            }
           }
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -698,14 +809,16 @@ bool make_map(CUtensorMap* map, CUtensorMapDataType type, uint32_t size, const v
                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-constexpr uint32_t kMaxPairs = 80;      // pieces of cut tiles at a time
-constexpr uint32_t kMinPieceSteps = 4;  // stages of a piece: shorter ones cost more in sums than they save
+constexpr uint32_t kMaxPairs = 80;
+constexpr uint32_t kMaxPieces = 160;    // sums of pieces that scratch has room for
+constexpr uint32_t kMinPieceSteps = 4;  // stages of a piece at the least
+constexpr uint32_t kSumSteps = 12;      // what a piece's sums cost, in stages: 128 KB out of every SM and in again
 
 }  // namespace
 
 uint64_t act_wgrad_scratch_bytes(uint64_t out_cols, uint64_t cols, uint32_t M) {
   (void)out_cols, (void)cols, (void)M;
-  return static_cast<uint64_t>(kMaxPairs) * kWgTile * kWgTile * sizeof(float);
+  return static_cast<uint64_t>(kMaxPieces) * kWgTile * kWgTile * sizeof(float);
 }
 
 int launch_act_wgrad(int dtype, const WgradArgs& a, const ActView& act, const RowShards& shards, unsigned int* status,
@@ -724,8 +837,13 @@ int launch_act_wgrad(int dtype, const WgradArgs& a, const ActView& act, const Ro
   const uint32_t pairs = min(kMaxPairs, static_cast<uint32_t>(shape.sm_count / 2));
   const uint32_t tiles = plan.tiles_n * plan.tiles_k * a.M, left = tiles % pairs;
   const uint32_t steps = static_cast<uint32_t>((shards.row0[plan.order[0] + 1] - shards.row0[plan.order[0]] + kWgRows - 1) / kWgRows);
-  plan.pieces = left ? min(pairs / left, steps / kMinPieceSteps) : 1u;
-  if (plan.pieces < 2) plan.pieces = 1;
+  // The cut that ends soonest: rounds of pieces, each with its stages and, when cut, its sums' way through scratch.
+  plan.pieces = 1;
+  uint64_t least = steps;
+  for (uint32_t p = 2; left && p <= steps / kMinPieceSteps && left * p <= kMaxPieces && p < 128; ++p) {
+    const uint64_t cost = static_cast<uint64_t>((left * p + pairs - 1) / pairs) * ((steps + p - 1) / p + kSumSteps);
+    if (cost < least) least = cost, plan.pieces = p;
+  }
   plan.whole = plan.pieces > 1 ? tiles - left : tiles;
   plan.units = plan.whole + plan.pieces * (tiles - plan.whole);
 
@@ -755,11 +873,11 @@ int launch_act_wgrad(int dtype, const WgradArgs& a, const ActView& act, const Ro
     }
     if (ok) launch_lm(kernel, grid, kWgThreads, smem, 1, stream, shape.chained, map_dy, map_codes, map_exps, plan, args, act.cols, status);
   };
-  if (tma && dtype == kDtypeBf16) go(std::integral_constant<int, 0>(), act_wgrad_kernel<__nv_bfloat16, true>, kWgSmem<1>);
-  else if (tma) go(std::integral_constant<int, 4>(), act_wgrad_kernel<__half, true>, kWgSmem<2>);
-  else if (dtype == kDtypeBf16) go(std::integral_constant<int, 1>(), act_wgrad_kernel<__nv_bfloat16, false>, kWgSmem<1>);
-  else if (dtype == kDtypeF16) go(std::integral_constant<int, 2>(), act_wgrad_kernel<__half, false>, kWgSmem<2>);
-  else go(std::integral_constant<int, 3>(), act_wgrad_kernel<float, false>, kWgSmem<3>);
+  if (tma && dtype == kDtypeBf16) go(std::integral_constant<int, 0>(), act_wgrad_kernel<__nv_bfloat16, true>, kWgSmem<__nv_bfloat16, true>);
+  else if (tma) go(std::integral_constant<int, 4>(), act_wgrad_kernel<__half, true>, kWgSmem<__half, true>);
+  else if (dtype == kDtypeBf16) go(std::integral_constant<int, 1>(), act_wgrad_kernel<__nv_bfloat16, false>, kWgSmem<__nv_bfloat16, false>);
+  else if (dtype == kDtypeF16) go(std::integral_constant<int, 2>(), act_wgrad_kernel<__half, false>, kWgSmem<__half, false>);
+  else go(std::integral_constant<int, 3>(), act_wgrad_kernel<float, false>, kWgSmem<float, false>);
   if (!ok) return -1;
   if (plan.pieces == 1) return 1;
   launch_lm(piece_sum_kernel, dim3((tiles - plan.whole) * 32), 256, 0, 1, stream, shape.chained, plan, a, act.cols);
