@@ -14,8 +14,9 @@
 //   0      issues the copies of dy, codes and exponent bytes (TMA, two rings of stages)
 //   1      issues the products (in the pair's first CTA)
 //   3      passes on that dy has landed, and clears what a ragged stage holds of the next worker's rows
+//   2, 3   or, where dy does not come by TMA, copy the aligned words around its rows
 //   4-11   add finished segments to fp32 sums in registers and write the tile
-//   12-19  convert codes, four warps a stage in turn
+//   12-19  convert codes, four warps a stage in turn (or four convert codes, and four shift and split dy)
 // Tensor memory holds two accumulators.  The tensor cores cut off what does not fit when they add to one: the
 // relative error grows by 8e-9 a product step (4.1e-6 after 8192 rows, in one go), so a segment ends after
 // kSegmentSteps steps and its sum is added in fp32 outside, rounded to nearest (error then as a plain fp32 product's).
@@ -59,7 +60,7 @@ template <> constexpr int kPieces<float> = 3;
 template <int kP, bool kTma> constexpr int kStages = kTma ? (kP == 1 ? 5 : 3) : kP == 1 ? 3 : 2;
 template <int kP> constexpr int kCodeStages = kP == 3 ? 3 : 4;
 template <int kP, bool kTma> constexpr int kHalves = kTma ? 0 : kP == 3 ? 3 : 8;
-constexpr int kHalfRows = kWgRows / 2;
+constexpr int kHalfRows = kWgRows / 2, kCopyThreads = 64;
 template <typename T> constexpr uint32_t kRawPitch = kWgHalf * sizeof(T) + 16;
 template <int kP> constexpr uint32_t kStageBytes = (kP + 1) * kOperandBytes;
 template <typename T, bool kTma>
@@ -344,15 +345,6 @@ __device__ __forceinline__ void next_half(HalfStage& h, const WgradPlan& plan, u
     enter_unit(h, plan, pairs);
   }
 }
-// Meeting of the group of four warps that brings dy; true if all of them say so.
-__device__ __forceinline__ bool group_agrees(bool ok) {
-  uint32_t all;
-  asm volatile(
-      "{\n.reg .pred p, q;\nsetp.ne.u32 q, %1, 0;\nbar.red.and.pred p, 1, %2, q;\nselp.u32 %0, 1, 0, p;\n}"
-      : "=r"(all) : "r"(static_cast<uint32_t>(ok)), "n"(kGroupWarps * 32) : "memory");
-  return all != 0;
-}
-
 // Rows of dy on any boundary, 128 columns from n0 + first on.
 template <typename T> struct DyRows {
   static constexpr uint32_t kVectors = kRawPitch<T> / 16;  // of 16 bytes around a row's 128 columns
@@ -363,9 +355,26 @@ template <typename T> struct DyRows {
   __device__ __forceinline__ const T* at(const HalfStage& h, uint32_t row) const {
     return dy + static_cast<uint64_t>(h.row + row) * ld + h.n0 + first;
   }
-  // Asks for a half's words, those that lie in the tensor and hold a column of it: four threads a row.
-  __device__ __forceinline__ void fetch(const HalfStage& h, uint32_t to, uint32_t ctid) const {
-    const uint32_t row = ctid >> 2, part = ctid & 3u;
+  // Asks for a half's words, those that lie in the tensor and hold a column of it.
+  __device__ __forceinline__ void fetch(const HalfStage& h, uint32_t to, uint32_t tid) const {
+    if (h.row >= 8 && h.row + kHalfRows <= h.end && h.n0 + first + kWgHalf + 16 / sizeof(T) <= n) {
+      // nothing to check: the lanes of a warp take neighbouring words, the last words of all rows come at the end
+      constexpr uint32_t kLanes = kVectors - 1, kAtOnce = kCopyThreads / kLanes;
+      const uint32_t row = tid / kLanes, v = tid % kLanes;
+      const T* begin = at(h, row);
+      uint32_t dst = to + row * kRawPitch<T> + v * 16;
+#pragma unroll
+      for (uint32_t i = 0; i < kHalfRows; i += kAtOnce, begin += kAtOnce * ld, dst += kAtOnce * kRawPitch<T>) {
+        const uintptr_t from = (reinterpret_cast<uintptr_t>(begin) & ~static_cast<uintptr_t>(15)) + v * 16;
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(from) : "memory");
+      }
+      if (tid < kHalfRows) {
+        const uintptr_t from = (reinterpret_cast<uintptr_t>(at(h, tid)) & ~static_cast<uintptr_t>(15)) + kLanes * 16;
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + tid * kRawPitch<T> + kLanes * 16), "l"(from) : "memory");
+      }
+      return;
+    }
+    const uint32_t row = tid >> 1, part = tid & 1u;
     if (h.row + row >= h.end || h.n0 + first >= n) return;
     const char* lo = reinterpret_cast<const char*>(dy);
     const char* hi = reinterpret_cast<const char*>(dy + (rows - 1) * ld + n);
@@ -373,16 +382,8 @@ template <typename T> struct DyRows {
     const char* end = reinterpret_cast<const char*>(begin + (n - h.n0 - first));  // of the row's columns
     const char* from = reinterpret_cast<const char*>(reinterpret_cast<uintptr_t>(begin) & ~static_cast<uintptr_t>(15)) + part * 16;
     uint32_t dst = to + row * kRawPitch<T> + part * 16;
-    if (from - part * 16 >= lo && from - part * 16 + kVectors * 16 <= end) {
-#pragma unroll
-      for (uint32_t v = 0; v + 1 < kVectors; v += 4)
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + v * 16), "l"(from + v * 16) : "memory");
-      if (part == 0)
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + (kVectors - 1) * 16), "l"(from + (kVectors - 1) * 16) : "memory");
-      return;
-    }
 #pragma unroll 1
-    for (uint32_t v = part; v < kVectors && from < end; v += 4, from += 64, dst += 64) {
+    for (uint32_t v = part; v < kVectors && from < end; v += 2, from += 32, dst += 32) {
       if (from >= lo) {
         const uint32_t bytes = hi - from < 16 ? static_cast<uint32_t>(hi - from) : 16u;
         asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(from), "r"(bytes) : "memory");
@@ -395,6 +396,7 @@ template <typename T> struct DyRows {
           else w[b / 4] |= static_cast<uint32_t>(*reinterpret_cast<const uint16_t*>(from + b)) << (8 * (b & 2));
         }
         store_shared(dst, make_uint4(w[0], w[1], w[2], w[3]));
+        __threadfence_block();
       }
     }
   }
@@ -406,16 +408,21 @@ template <typename T> struct DyRows {
     uint32_t shift = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(at(h, r0)));
     uint32_t from = raw + r0 * kRawPitch<T> + chunk * (kUnit * sizeof(T)), out = to + chunk_offset(h.half * kHalfRows + r0, chunk);
     const uint32_t valid = c < n && h.row + r0 < h.end ? h.end - h.row - r0 : 0u;  // rows from r0 on
+    constexpr uint32_t kTogether = sizeof(T) == 4 ? 2 : 4;  // rows whose words are loaded together
+    uint32_t words[kTogether][kWords + 4];
 #pragma unroll
     for (uint32_t i = 0; i < kHalfRows / 8; ++i) {
-      uint32_t x[kWords + 4];
-      Unit<T> u;
+      if (i % kTogether == 0) {
 #pragma unroll
-      for (int k = 0; k < kWords / 4 + 1; ++k) {
-        const uint4 v = load_shared(from + i * 8 * kRawPitch<T> + k * 16);
-        x[4 * k] = v.x, x[4 * k + 1] = v.y, x[4 * k + 2] = v.z, x[4 * k + 3] = v.w;
+        for (uint32_t l = 0; l < kTogether; ++l)
+#pragma unroll
+          for (int k = 0; k < kWords / 4 + 1; ++k) {
+            const uint4 v = load_shared(from + (i + l) * 8 * kRawPitch<T> + k * 16);
+            words[l][4 * k] = v.x, words[l][4 * k + 1] = v.y, words[l][4 * k + 2] = v.z, words[l][4 * k + 3] = v.w;
+          }
       }
-      shifted_words<kWords>(x, (shift + i * 8 * pitch) & 15u, u.w);
+      Unit<T> u;
+      shifted_words<kWords>(words[i % kTogether], (shift + i * 8 * pitch) & 15u, u.w);
       if (8 * i >= valid) {
 #pragma unroll
         for (int k = 0; k < kWords; ++k) u.w[k] = 0u;
@@ -444,7 +451,7 @@ act_wgrad_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_consta
   constexpr uint32_t kStage = kStageBytes<kP>;
   constexpr int kSegment = kSegmentSteps / (kWgRows / 16) / kP;  // stages of a segment
   extern __shared__ uint8_t smem_raw[];
-  __shared__ __align__(8) uint64_t bars[3 * kN + 2 * kC + 4];
+  __shared__ __align__(8) uint64_t bars[3 * kN + 2 * kC + 4 + 2 * kRaw];
   __shared__ uint32_t tmem_base, gave_up, last_at, last_phase;
   const uint32_t tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   uint32_t rank;
@@ -455,7 +462,7 @@ act_wgrad_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_consta
   // full: a copy has landed in this CTA (of dy, of codes); ready: both CTAs' part of a stage can be multiplied (the
   // first CTA's barriers count); empty: a stage may be overwritten
   const uint32_t full = smem_addr(bars), ready = full + 8 * kN, empty = ready + 8 * kN, code_full = empty + 8 * kN,
-                 code_empty = code_full + 8 * kC, acc_full = code_empty + 8 * kC, acc_empty = acc_full + 16;
+                 code_empty = code_full + 8 * kC, acc_full = code_empty + 8 * kC, acc_empty = acc_full + 16, raw_full = acc_empty + 16, raw_empty = raw_full + 8 * kRaw;
   if (tid == 0) {
     gave_up = 0u;
     for (int s = 0; s < kN; ++s) {
@@ -466,6 +473,10 @@ act_wgrad_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_consta
     for (int s = 0; s < kC; ++s) {
       barrier_init(code_full + 8 * s, 1);
       barrier_init(code_empty + 8 * s, kGroupWarps);
+    }
+    for (int i = 0; i < kRaw; ++i) {
+      barrier_init(raw_full + 8 * i, kCopyThreads);
+      barrier_init(raw_empty + 8 * i, kGroupWarps);
     }
     for (int i = 0; i < 2; ++i) {
       barrier_init(acc_full + 8 * i, 1);
@@ -594,6 +605,18 @@ act_wgrad_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_consta
           rows -= min(rows, static_cast<uint32_t>(kWgRows));
         }
       }
+    } else if (!kTma && warp >= 2) {
+      // copies of dy
+      if constexpr (!kTma) {
+        const DyRows<T> from = {static_cast<const T*>(a.dy), a.ld_dy, a.rows, a.out_cols, rank * kWgHalf};
+        Ring<kRaw> raw = {0, 0};
+        for (HalfStage h = first_half(plan, pair, pairs); h.u < plan.units; next_half(h, plan, pairs), raw.next()) {
+          if (!all_wait(raw_empty + 8 * raw.at, raw.phase ^ 1u, &gave_up)) break;
+          from.fetch(h, at_raw + raw.at * kHalfRows * kRawPitch<T>, tid - 64);
+          asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(raw_full + 8 * raw.at) : "memory");
+        }
+        asm volatile("cp.async.wait_all;" ::: "memory");
+      }
     }
   } else if (warp >= kFirstConvert) {
     // conversion: by TMA the groups of warps take stages in turn, otherwise one brings dy and the other converts codes
@@ -606,37 +629,26 @@ act_wgrad_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_consta
     const uint32_t to0 = chunk_offset(r0, second * 8 + seg), to1 = to0 ^ kAtomBytes;
     const uint32_t byte0 = 0x4440u + second * 2 + (seg >> 2), byte1 = byte0 ^ 2u;  // their exponent bytes in a row's word
     const T* dy = static_cast<const T*>(a.dy);
-    const uint32_t ready_of_first = map_rank(ready, 0), code_empty_own = map_rank(code_empty, rank);
+    const uint32_t ready_of_first = map_rank(ready, 0), code_empty_own = map_rank(code_empty, rank), raw_empty_own = map_rank(raw_empty, rank);
     Ring<kN> r = {0, 0};
     if constexpr (!kTma) {
       if (group == 1) {  // dy
         const DyRows<T> from = {dy, a.ld_dy, a.rows, a.out_cols, rank * kWgHalf};
-        HalfStage ahead = first_half(plan, pair, pairs), now = ahead;
-        auto fetch = [&](uint32_t buffer) {
-          if (ahead.u < plan.units) {
-            from.fetch(ahead, at_raw + buffer * kHalfRows * kRawPitch<T>, ctid);
-            next_half(ahead, plan, pairs);
-          }
-          asm volatile("cp.async.commit_group;" ::: "memory");
-        };
-        for (uint32_t i = 0; i + 1 < kRaw; ++i) fetch(i);
+        Ring<kRaw> raw = {0, 0};
         bool ok = true;
-        for (uint32_t buffer = 0; now.u < plan.units; buffer = buffer + 1 == kRaw ? 0 : buffer + 1) {
-          asm volatile("cp.async.wait_group %0;" ::"n"(kRaw - 2) : "memory");
-          // every warp's words of this half have landed, and everybody is done with the half before: its place is free
-          if (!(ok = group_agrees(ok))) break;
-          fetch(buffer == 0 ? kRaw - 1 : buffer - 1);
-          if (now.half == 0) ok = all_wait(empty + 8 * r.at, r.phase ^ 1u, &gave_up);
-          if (ok) from.finish(now, at_raw + buffer * kHalfRows * kRawPitch<T>, at_ring + r.at * kStage, ctid);
-          if (now.half == 1) {
+        for (HalfStage h = first_half(plan, pair, pairs); h.u < plan.units; next_half(h, plan, pairs), raw.next()) {
+          if (h.half == 0 && !(ok = all_wait(empty + 8 * r.at, r.phase ^ 1u, &gave_up))) break;
+          if (!(ok = all_wait(raw_full + 8 * raw.at, raw.phase, &gave_up))) break;
+          from.finish(h, at_raw + raw.at * kHalfRows * kRawPitch<T>, at_ring + r.at * kStage, ctid);
+          __syncwarp();
+          if (lane == 0) barrier_arrive_cluster(raw_empty_own + 8 * raw.at);
+          if (h.half == 1) {
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
-            if (ok && lane == 0) barrier_arrive_cluster(ready_of_first + 8 * r.at);
+            if (lane == 0) barrier_arrive_cluster(ready_of_first + 8 * r.at);
             r.next();
           }
-          next_half(now, plan, pairs);
         }
-        asm volatile("cp.async.wait_all;" ::: "memory");
       }
     }
     Ring<kC> rc = {0, 0};
