@@ -898,7 +898,7 @@ qasg_status qasg_act_wgrad(qasg_ctx* ctx, qasg_dtype dtype, const void* dy, uint
   if ((st = enter(ctx)) != QASG_OK) return st;
   WgradArgs a;
   a.dy = dy, a.weight = weight, a.g = g, a.scratch = scratch, a.scratch_bytes = scratch_bytes;
-  a.ld_dy = ld_dy, a.ld_g = ld_g, a.ld_w = ld_w, a.rows = view.rows, a.out_cols = static_cast<uint32_t>(out_cols), a.M = M, a.device = ctx->device;
+  a.ld_dy = ld_dy, a.ld_g = ld_g, a.ld_w = ld_w, a.out_cols = static_cast<uint32_t>(out_cols), a.M = M, a.device = ctx->device;
   a.accumulate = accumulate != 0;
   {
     Launch l(ctx, kActWgrad, static_cast<cudaStream_t>(stream));

@@ -247,7 +247,7 @@ struct WgradArgs {
   const float* weight;  // NULL: ones; one factor per column of the checkpoint
   float* g;             // worker m's gradient at g + m * ld_g, row n at + n * ld_w
   void* scratch;
-  uint64_t scratch_bytes, ld_dy, ld_g, ld_w, rows;
+  uint64_t scratch_bytes, ld_dy, ld_g, ld_w;
   uint32_t out_cols, M;
   int device;
   int vector;  // floats of g that lie aligned together: 4, 2 or 1; set by the launcher

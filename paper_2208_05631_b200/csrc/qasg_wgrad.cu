@@ -14,9 +14,8 @@
 //   0      issues the copies of dy, codes and exponent bytes (TMA, two rings of stages)
 //   1      issues the products (in the pair's first CTA)
 //   3      passes on that dy has landed, and clears what a ragged stage holds of the next worker's rows
-//   2, 3   or, where dy does not come by TMA, copy the aligned words around its rows
 //   4-11   add finished segments to fp32 sums in registers and write the tile
-//   12-19  convert codes, four warps a stage in turn (or four convert codes, and four shift and split dy)
+//   12-19  convert codes, four warps a stage in turn
 // Tensor memory holds two accumulators.  The tensor cores cut off what does not fit when they add to one: the
 // relative error grows by 8e-9 a product step (4.1e-6 after 8192 rows, in one go), so a segment ends after
 // kSegmentSteps steps and its sum is added in fp32 outside, rounded to nearest (error then as a plain fp32 product's).
@@ -49,23 +48,18 @@ constexpr uint32_t kAtomBytes = kWgRows * 128;             // 64 columns x 64 ro
 constexpr int kTurnCols = 16, kTurnPitch = 20;  // floats: rows of whole 16-byte words over all banks
 constexpr long long kMaxWait = 1ll << 34;                  // bound of every wait in cycles (some seconds)
 
-// How dy reaches shared memory, as 1, 2 or 3 bf16 pieces: 16-bit rows on 16-byte boundaries by TMA (fp16 is then split
-// in place by the converting warps); everything else in the aligned words around each row (cp.async), which four of the
-// converting warps shift and split.
+// dy is read by TMA as one plane of bf16, which takes rows on 16-byte boundaries: its own, if it is bf16 and they are,
+// else planes in scratch that another launch has written, 1 (bf16), 2 (fp16) or 3 (fp32) of them, one below the other.
+// (Shifting and splitting rows inside this kernel, by asynchronous copies and four of the converting warps, took twice
+// as long as both launches: 4031 x 3072 x 2300 fp16 190 us.)
 template <typename T> constexpr int kPieces = 1;
 template <> constexpr int kPieces<__half> = 2;
 template <> constexpr int kPieces<float> = 3;
-// Stages of the two rings: operands (the pieces of dy, then the converted codes), and codes as they come; and, where
-// dy does not come by TMA, the halves of a stage (32 rows, in the aligned words around them) that are on their way.
-template <int kP, bool kTma> constexpr int kStages = kTma ? (kP == 1 ? 5 : 3) : kP == 1 ? 3 : 2;
-template <int kP> constexpr int kCodeStages = kP == 3 ? 3 : 4;
-template <int kP, bool kTma> constexpr int kHalves = kTma ? 0 : kP == 3 ? 3 : 8;
-constexpr int kHalfRows = kWgRows / 2, kCopyThreads = 64;
-template <typename T> constexpr uint32_t kRawPitch = kWgHalf * sizeof(T) + 16;
+// Stages of the two rings: operands (the pieces of dy, then the converted codes), and codes as they come.
+template <int kP> constexpr int kStages = kP == 1 ? 5 : kP == 2 ? 3 : 2;
+constexpr int kCodeStages = 4;
 template <int kP> constexpr uint32_t kStageBytes = (kP + 1) * kOperandBytes;
-template <typename T, bool kTma>
-constexpr uint32_t kWgSmem = kStages<kPieces<T>, kTma> * kStageBytes<kPieces<T>> + kCodeStages<kPieces<T>> * kCodeStage +
-                             kHalves<kPieces<T>, kTma> * kHalfRows * kRawPitch<T> + 8 * 32 * kTurnPitch * 4 + 1024;
+template <int kP> constexpr uint32_t kWgSmem = kStages<kP> * kStageBytes<kP> + kCodeStages * kCodeStage + 8 * 32 * kTurnPitch * 4 + 1024;
 
 struct WgradPlan {
   uint32_t row0[kMaxWorkers + 1];
@@ -73,6 +67,7 @@ struct WgradPlan {
   uint32_t tiles_n, tiles_k;    // per worker
   uint32_t whole;               // tiles summed by one pair each; the tiles after them are cut into pieces
   uint32_t pieces, units;       // units = whole + pieces * (tiles - whole)
+  uint32_t plane_row0, plane_rows;  // the planes of dy begin with this row, and hold so many
 };
 
 // ------------------------------------------------------------------ PTX
@@ -241,11 +236,6 @@ __device__ __forceinline__ uint32_t chunk_offset(uint32_t t, uint32_t chunk) {
 __device__ __forceinline__ void store_shared(uint32_t addr, uint4 v) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
-__device__ __forceinline__ uint4 load_shared(uint32_t addr) {
-  uint4 v;
-  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
-  return v;
-}
 __device__ __forceinline__ uint2 load_shared2(uint32_t addr) {
   uint2 v;
   asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr) : "memory");
@@ -301,182 +291,81 @@ __device__ __forceinline__ void store_sums(float* turn, uint32_t lane, const flo
   }
 }
 
+// ------------------------------------------------------------------ planes of dy
 // The leading eight bits of eight values as bf16; v becomes what is left (nothing of an infinity).
-__device__ __forceinline__ uint4 leading_bits(float (&v)[kUnit]) {
-  uint32_t q[4];
+__device__ __forceinline__ Unit<__nv_bfloat16> leading_bits(float (&v)[kUnit]) {
+  Unit<__nv_bfloat16> u;
 #pragma unroll
-  for (int j = 0; j < 4; ++j) q[j] = __byte_perm(__float_as_uint(v[2 * j]), __float_as_uint(v[2 * j + 1]), 0x7632);
-  float most = 0.f, rest[kUnit];
+  for (int j = 0; j < 4; ++j) u.w[j] = __byte_perm(__float_as_uint(v[2 * j]), __float_as_uint(v[2 * j + 1]), 0x7632);
 #pragma unroll
   for (int j = 0; j < kUnit; ++j) {
-    most = fmaxf(most, fabsf(v[j]));
-    rest[j] = v[j] - __uint_as_float(__float_as_uint(v[j]) & 0xffff0000u);
+    const float rest = v[j] - __uint_as_float(__float_as_uint(v[j]) & 0xffff0000u);
+    v[j] = fabsf(v[j]) == INFINITY ? 0.f : rest;
   }
-  if (most == INFINITY) {
-#pragma unroll
-    for (int j = 0; j < kUnit; ++j) rest[j] = fabsf(v[j]) == INFINITY ? 0.f : rest[j];
-  }
-#pragma unroll
-  for (int j = 0; j < kUnit; ++j) v[j] = rest[j];
-  return make_uint4(q[0], q[1], q[2], q[3]);
+  return u;
 }
 
-// The halves of stages, in the order in which a pair works on them.
-struct HalfStage {
-  uint32_t u, row, end, n0, half;  // unit; first row of the half, end of the unit's rows; first column; 0 or 1
-};
-__device__ __forceinline__ void enter_unit(HalfStage& h, const WgradPlan& plan, uint32_t pairs) {
-  for (; h.u < plan.units; h.u += pairs) {  // the next unit that has rows
-    const TileWork w = unit_of(plan, h.u);
-    h.row = w.row0, h.end = w.row1, h.n0 = w.n0, h.half = 0;
-    if (w.row0 < w.row1) return;
+// Rows row0 to row0 + rows - 1 of dy as kPieces<T> planes of bf16 with rows of ld_plane (a multiple of 8) values, zeros
+// behind column n.  Elementwise, bound by HBM; a warp takes 1024 columns of a row, a lane four units.
+constexpr int kSplitUnits = 4, kSplitWarps = 8;
+template <typename T, bool kAligned>
+__global__ void __launch_bounds__(32 * kSplitWarps)
+split_rows_kernel(const T* dy, uint64_t ld, uint64_t all_rows, uint64_t row0, uint32_t rows, uint32_t n, __nv_bfloat16* planes,
+                  uint32_t ld_plane, uint32_t per_row) {
+  const uint64_t item = static_cast<uint64_t>(blockIdx.x) * kSplitWarps + (threadIdx.x >> 5);
+  chain_wait();
+  chain_trigger();
+  const uint64_t row = item / per_row;
+  if (row >= rows) return;
+  const uint32_t c0 = (static_cast<uint32_t>(item - row * per_row) * 32 * kSplitUnits + (threadIdx.x & 31)) * kUnit;
+  const T* from = dy + (row0 + row) * ld;
+  const Extent tensor = extent_of(dy, all_rows, ld, n);
+  Fetched<T, kAligned> f[kSplitUnits];
+#pragma unroll
+  for (int j = 0; j < kSplitUnits; ++j) f[j] = fetch_unit<T, kAligned>(from, row0 + row, c0 + j * 32 * kUnit, n, tensor);
+#pragma unroll
+  for (int j = 0; j < kSplitUnits; ++j) {
+    const uint32_t c = c0 + j * 32 * kUnit;
+    if (c >= ld_plane) continue;
+    float v[kUnit];
+    unit_floats(finish_unit(f[j], from, c, n), v);
+#pragma unroll
+    for (int p = 0; p < kPieces<T>; ++p) store_unit(planes + (static_cast<uint64_t>(p) * rows + row) * ld_plane + c, leading_bits(v));
   }
 }
-__device__ __forceinline__ HalfStage first_half(const WgradPlan& plan, uint32_t pair, uint32_t pairs) {
-  HalfStage h = {pair, 0, 0, 0, 0};
-  enter_unit(h, plan, pairs);
-  return h;
-}
-__device__ __forceinline__ void next_half(HalfStage& h, const WgradPlan& plan, uint32_t pairs) {
-  h.row += kHalfRows;
-  h.half ^= 1u;
-  if (h.half == 0 && h.row >= h.end) {
-    h.u += pairs;
-    enter_unit(h, plan, pairs);
-  }
-}
-// Rows of dy on any boundary, 128 columns from n0 + first on.
-template <typename T> struct DyRows {
-  static constexpr uint32_t kVectors = kRawPitch<T> / 16;  // of 16 bytes around a row's 128 columns
-  const T* dy;
-  uint64_t ld, rows;
-  uint32_t n, first;
-
-  __device__ __forceinline__ const T* at(const HalfStage& h, uint32_t row) const {
-    return dy + static_cast<uint64_t>(h.row + row) * ld + h.n0 + first;
-  }
-  // Asks for a half's words, those that lie in the tensor and hold a column of it.
-  __device__ __forceinline__ void fetch(const HalfStage& h, uint32_t to, uint32_t tid) const {
-    if (h.row >= 8 && h.row + kHalfRows <= h.end && h.n0 + first + kWgHalf + 16 / sizeof(T) <= n) {
-      // nothing to check: the lanes of a warp take neighbouring words, the last words of all rows come at the end
-      constexpr uint32_t kLanes = kVectors - 1, kAtOnce = kCopyThreads / kLanes;
-      const uint32_t row = tid / kLanes, v = tid % kLanes;
-      const T* begin = at(h, row);
-      uint32_t dst = to + row * kRawPitch<T> + v * 16;
-#pragma unroll
-      for (uint32_t i = 0; i < kHalfRows; i += kAtOnce, begin += kAtOnce * ld, dst += kAtOnce * kRawPitch<T>) {
-        const uintptr_t from = (reinterpret_cast<uintptr_t>(begin) & ~static_cast<uintptr_t>(15)) + v * 16;
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(from) : "memory");
-      }
-      if (tid < kHalfRows) {
-        const uintptr_t from = (reinterpret_cast<uintptr_t>(at(h, tid)) & ~static_cast<uintptr_t>(15)) + kLanes * 16;
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + tid * kRawPitch<T> + kLanes * 16), "l"(from) : "memory");
-      }
-      return;
-    }
-    const uint32_t row = tid >> 1, part = tid & 1u;
-    if (h.row + row >= h.end || h.n0 + first >= n) return;
-    const char* lo = reinterpret_cast<const char*>(dy);
-    const char* hi = reinterpret_cast<const char*>(dy + (rows - 1) * ld + n);
-    const T* begin = at(h, row);
-    const char* end = reinterpret_cast<const char*>(begin + (n - h.n0 - first));  // of the row's columns
-    const char* from = reinterpret_cast<const char*>(reinterpret_cast<uintptr_t>(begin) & ~static_cast<uintptr_t>(15)) + part * 16;
-    uint32_t dst = to + row * kRawPitch<T> + part * 16;
-#pragma unroll 1
-    for (uint32_t v = part; v < kVectors && from < end; v += 2, from += 32, dst += 32) {
-      if (from >= lo) {
-        const uint32_t bytes = hi - from < 16 ? static_cast<uint32_t>(hi - from) : 16u;
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(from), "r"(bytes) : "memory");
-      } else {  // the words the tensor begins in
-        uint32_t w[4] = {0u, 0u, 0u, 0u};
-#pragma unroll
-        for (int b = 0; b < 16; b += sizeof(T)) {
-          if (from + b < lo || from + b >= hi) continue;
-          if (sizeof(T) == 4) w[b / 4] = *reinterpret_cast<const uint32_t*>(from + b);
-          else w[b / 4] |= static_cast<uint32_t>(*reinterpret_cast<const uint16_t*>(from + b)) << (8 * (b & 2));
-        }
-        store_shared(dst, make_uint4(w[0], w[1], w[2], w[3]));
-        __threadfence_block();
-      }
-    }
-  }
-  // Shifts and splits a half that has landed: a thread takes a chunk of eight columns of rows r, r + 8, ...
-  __device__ __forceinline__ void finish(const HalfStage& h, uint32_t raw, uint32_t to, uint32_t ctid) const {
-    constexpr int kWords = sizeof(Unit<T>) / 4;
-    const uint32_t chunk = ctid & 15u, c = h.n0 + first + chunk * kUnit, r0 = ctid >> 4;
-    const uint32_t pitch = static_cast<uint32_t>(ld * sizeof(T));  // the low bits decide a row's shift
-    uint32_t shift = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(at(h, r0)));
-    uint32_t from = raw + r0 * kRawPitch<T> + chunk * (kUnit * sizeof(T)), out = to + chunk_offset(h.half * kHalfRows + r0, chunk);
-    const uint32_t valid = c < n && h.row + r0 < h.end ? h.end - h.row - r0 : 0u;  // rows from r0 on
-    constexpr uint32_t kTogether = sizeof(T) == 4 ? 2 : 4;  // rows whose words are loaded together
-    uint32_t words[kTogether][kWords + 4];
-#pragma unroll
-    for (uint32_t i = 0; i < kHalfRows / 8; ++i) {
-      if (i % kTogether == 0) {
-#pragma unroll
-        for (uint32_t l = 0; l < kTogether; ++l)
-#pragma unroll
-          for (int k = 0; k < kWords / 4 + 1; ++k) {
-            const uint4 v = load_shared(from + (i + l) * 8 * kRawPitch<T> + k * 16);
-            words[l][4 * k] = v.x, words[l][4 * k + 1] = v.y, words[l][4 * k + 2] = v.z, words[l][4 * k + 3] = v.w;
-          }
-      }
-      Unit<T> u;
-      shifted_words<kWords>(words[i % kTogether], (shift + i * 8 * pitch) & 15u, u.w);
-      if (8 * i >= valid) {
-#pragma unroll
-        for (int k = 0; k < kWords; ++k) u.w[k] = 0u;
-      } else if (c + kUnit > n) {
-        clear_past(u, c, n);
-      }
-      if constexpr (kPieces<T> == 1) {
-        store_shared(out + i * 1024, make_uint4(u.w[0], u.w[1], u.w[2], u.w[3]));
-      } else {
-        float v[kUnit];
-        unit_floats(u, v);
-#pragma unroll
-        for (int p = 0; p < kPieces<T>; ++p) store_shared(out + p * kOperandBytes + i * 1024, leading_bits(v));
-      }
-    }
-  }
-};
 
 // ------------------------------------------------------------------ kernel
-template <typename T, bool kTma>
+template <int kP>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWgThreads, 1)
 act_wgrad_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_constant__ CUtensorMap map_codes,
                  const __grid_constant__ CUtensorMap map_exps, const __grid_constant__ WgradPlan plan,
                  const __grid_constant__ WgradArgs a, uint32_t cols, unsigned int* __restrict__ status) {
-  constexpr int kP = kPieces<T>, kN = kStages<kP, kTma>, kC = kCodeStages<kP>, kRaw = kHalves<kP, kTma>;
+  constexpr int kN = kStages<kP>, kC = kCodeStages;
   constexpr uint32_t kStage = kStageBytes<kP>;
   constexpr int kSegment = kSegmentSteps / (kWgRows / 16) / kP;  // stages of a segment
   extern __shared__ uint8_t smem_raw[];
-  __shared__ __align__(8) uint64_t bars[3 * kN + 2 * kC + 4 + 2 * kRaw];
+  __shared__ __align__(8) uint64_t bars[3 * kN + 2 * kC + 4];
   __shared__ uint32_t tmem_base, gave_up, last_at, last_phase;
   const uint32_t tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   uint32_t rank;
   asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
   const uint32_t pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
   const uint32_t at_ring = (smem_addr(smem_raw) + 1023u) & ~1023u, at_codes = at_ring + kN * kStage,
-                 at_turn = at_codes + kC * kCodeStage, at_raw = at_turn + 8 * 32 * kTurnPitch * 4;
+                 at_turn = at_codes + kC * kCodeStage;
   // full: a copy has landed in this CTA (of dy, of codes); ready: both CTAs' part of a stage can be multiplied (the
   // first CTA's barriers count); empty: a stage may be overwritten
   const uint32_t full = smem_addr(bars), ready = full + 8 * kN, empty = ready + 8 * kN, code_full = empty + 8 * kN,
-                 code_empty = code_full + 8 * kC, acc_full = code_empty + 8 * kC, acc_empty = acc_full + 16, raw_full = acc_empty + 16, raw_empty = raw_full + 8 * kRaw;
+                 code_empty = code_full + 8 * kC, acc_full = code_empty + 8 * kC, acc_empty = acc_full + 16;
   if (tid == 0) {
     gave_up = 0u;
     for (int s = 0; s < kN; ++s) {
       barrier_init(full + 8 * s, 1);
-      barrier_init(ready + 8 * s, 2 * kGroupWarps + (!kTma ? 2 * kGroupWarps : kP == 1 ? 2 : 0));
+      barrier_init(ready + 8 * s, 2 * kGroupWarps + 2);
       barrier_init(empty + 8 * s, 1);
     }
     for (int s = 0; s < kC; ++s) {
       barrier_init(code_full + 8 * s, 1);
       barrier_init(code_empty + 8 * s, kGroupWarps);
-    }
-    for (int i = 0; i < kRaw; ++i) {
-      barrier_init(raw_full + 8 * i, kCopyThreads);
-      barrier_init(raw_empty + 8 * i, kGroupWarps);
     }
     for (int i = 0; i < 2; ++i) {
       barrier_init(acc_full + 8 * i, 1);
@@ -522,16 +411,18 @@ act_wgrad_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_consta
             tma_load(at + kCodeBytes, &map_exps, (k / kActBlock) & ~15, y, bar);
           }
           rc.next();
-          if (kTma) {
-            if (!(ok = all_wait(empty + 8 * r.at, r.phase ^ 1u, &gave_up))) break;
-            if (one) {
-              const uint32_t bar = full + 8 * r.at, at = at_ring + r.at * kStage;
-              barrier_expect(bar, kOperandBytes);
-              tma_load(at, &map_dy, n, y, bar);
-              tma_load(at + kAtomBytes, &map_dy, n + 64, y, bar);
+          if (!(ok = all_wait(empty + 8 * r.at, r.phase ^ 1u, &gave_up))) break;
+          if (one) {
+            const uint32_t bar = full + 8 * r.at, at = at_ring + r.at * kStage;
+            barrier_expect(bar, kP * kOperandBytes);
+#pragma unroll
+            for (int p = 0; p < kP; ++p) {
+              const int in_plane = static_cast<int>(y - plan.plane_row0 + p * plan.plane_rows);
+              tma_load(at + p * kOperandBytes, &map_dy, n, in_plane, bar);
+              tma_load(at + p * kOperandBytes + kAtomBytes, &map_dy, n + 64, in_plane, bar);
             }
-            r.next();
           }
+          r.next();
           ++issued;
         }
       }
@@ -540,7 +431,7 @@ act_wgrad_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_consta
           rc.back();
           barrier_drain(code_full + 8 * rc.at, rc.phase);
         }
-        for (uint32_t i = kTma ? min(issued, static_cast<uint32_t>(kN)) : 0; i > 0; --i) {
+        for (uint32_t i = min(issued, static_cast<uint32_t>(kN)); i > 0; --i) {
           r.back();
           barrier_drain(full + 8 * r.at, r.phase);
         }
@@ -585,7 +476,7 @@ act_wgrad_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_consta
         }
       }
       if (lane == 0) last_at = r.at, last_phase = r.phase;
-    } else if (warp == 3 && kTma && kP == 1) {
+    } else if (warp == 3) {
       Ring<kN> r = {0, 0};
       const uint32_t ready_of_first = map_rank(ready, 0);
       bool ok = true;
@@ -595,8 +486,9 @@ act_wgrad_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_consta
         while (rows) {
           if (!(ok = all_wait(full + 8 * r.at, r.phase, &gave_up))) break;
           if (rows < kWgRows) {  // rows of another worker came with the copy: they must not meet 0 * inf
-            for (uint32_t i = lane; i < (kWgRows - rows) * 16; i += 32)
-              store_shared(at_ring + r.at * kStage + chunk_offset(rows + (i >> 4), i & 15u), make_uint4(0u, 0u, 0u, 0u));
+            for (int p = 0; p < kP; ++p)
+              for (uint32_t i = lane; i < (kWgRows - rows) * 16; i += 32)
+                store_shared(at_ring + r.at * kStage + p * kOperandBytes + chunk_offset(rows + (i >> 4), i & 15u), make_uint4(0u, 0u, 0u, 0u));
           }
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
@@ -605,21 +497,9 @@ act_wgrad_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_consta
           rows -= min(rows, static_cast<uint32_t>(kWgRows));
         }
       }
-    } else if (!kTma && warp >= 2) {
-      // copies of dy
-      if constexpr (!kTma) {
-        const DyRows<T> from = {static_cast<const T*>(a.dy), a.ld_dy, a.rows, a.out_cols, rank * kWgHalf};
-        Ring<kRaw> raw = {0, 0};
-        for (HalfStage h = first_half(plan, pair, pairs); h.u < plan.units; next_half(h, plan, pairs), raw.next()) {
-          if (!all_wait(raw_empty + 8 * raw.at, raw.phase ^ 1u, &gave_up)) break;
-          from.fetch(h, at_raw + raw.at * kHalfRows * kRawPitch<T>, tid - 64);
-          asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(raw_full + 8 * raw.at) : "memory");
-        }
-        asm volatile("cp.async.wait_all;" ::: "memory");
-      }
     }
   } else if (warp >= kFirstConvert) {
-    // conversion: by TMA the groups of warps take stages in turn, otherwise one brings dy and the other converts codes
+    // conversion: the groups of warps take stages in turn
     fewer_registers<kConvertRegs>();
     const uint32_t group = (warp - kFirstConvert) / kGroupWarps, ctid = tid - (kFirstConvert + group * kGroupWarps) * 32;
     // a thread takes eight columns (seg) of either atom in rows r0, r0 + 16, ...; threads of odd rows take the
@@ -628,37 +508,16 @@ act_wgrad_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_consta
     const uint32_t from0 = r0 * kWgHalf + second * 64 + seg * 8, from1 = from0 ^ 64u;
     const uint32_t to0 = chunk_offset(r0, second * 8 + seg), to1 = to0 ^ kAtomBytes;
     const uint32_t byte0 = 0x4440u + second * 2 + (seg >> 2), byte1 = byte0 ^ 2u;  // their exponent bytes in a row's word
-    const T* dy = static_cast<const T*>(a.dy);
-    const uint32_t ready_of_first = map_rank(ready, 0), code_empty_own = map_rank(code_empty, rank), raw_empty_own = map_rank(raw_empty, rank);
+    const uint32_t ready_of_first = map_rank(ready, 0), code_empty_own = map_rank(code_empty, rank);
     Ring<kN> r = {0, 0};
-    if constexpr (!kTma) {
-      if (group == 1) {  // dy
-        const DyRows<T> from = {dy, a.ld_dy, a.rows, a.out_cols, rank * kWgHalf};
-        Ring<kRaw> raw = {0, 0};
-        bool ok = true;
-        for (HalfStage h = first_half(plan, pair, pairs); h.u < plan.units; next_half(h, plan, pairs), raw.next()) {
-          if (h.half == 0 && !(ok = all_wait(empty + 8 * r.at, r.phase ^ 1u, &gave_up))) break;
-          if (!(ok = all_wait(raw_full + 8 * raw.at, raw.phase, &gave_up))) break;
-          from.finish(h, at_raw + raw.at * kHalfRows * kRawPitch<T>, at_ring + r.at * kStage, ctid);
-          __syncwarp();
-          if (lane == 0) barrier_arrive_cluster(raw_empty_own + 8 * raw.at);
-          if (h.half == 1) {
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            __syncwarp();
-            if (lane == 0) barrier_arrive_cluster(ready_of_first + 8 * r.at);
-            r.next();
-          }
-        }
-      }
-    }
     Ring<kC> rc = {0, 0};
     uint32_t turn = 0;
     bool ok = true;
-    for (uint32_t u = pair; u < plan.units && ok && (kTma || group == 0); u += pairs) {
+    for (uint32_t u = pair; u < plan.units && ok; u += pairs) {
       const TileWork w = unit_of(plan, u);
       const uint32_t exp_at = ((w.k0 + rank * kWgHalf) / kActBlock) & 15u;  // four blocks: one word
       for (uint32_t t = w.row0; t < w.row1; t += kWgRows, r.next(), rc.next(), turn ^= 1u) {
-        if (kTma && turn != group) continue;
+        if (turn != group) continue;
         const uint32_t rows = min(static_cast<uint32_t>(kWgRows), w.row1 - t);
         if (!(ok = all_wait(code_full + 8 * rc.at, rc.phase, &gave_up))) break;
         if (!(ok = all_wait(empty + 8 * r.at, r.phase ^ 1u, &gave_up))) break;
@@ -684,21 +543,6 @@ act_wgrad_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_consta
               store_shared(out + to0 + i * 2048, make_uint4(0u, 0u, 0u, 0u));
               store_shared(out + to1 + i * 2048, make_uint4(0u, 0u, 0u, 0u));
             }
-        }
-        if (kTma && kP == 2) {
-          if (!(ok = all_wait(full + 8 * r.at, r.phase, &gave_up))) break;
-#pragma unroll 2
-          for (int i = 0; i < 8; ++i) {
-            const uint32_t y = (ctid >> 4) + 8 * i, at = stage + chunk_offset(y, ctid & 15u);
-            uint4 q = load_shared(at);
-            if (y >= rows) q = make_uint4(0u, 0u, 0u, 0u);  // rows of another worker came with the copy
-            Unit<T> u;
-            u.w[0] = q.x, u.w[1] = q.y, u.w[2] = q.z, u.w[3] = q.w;
-            float v[kUnit];
-            unit_floats(u, v);
-            store_shared(at, leading_bits(v));
-            store_shared(at + kOperandBytes, leading_bits(v));
-          }
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
@@ -822,33 +666,46 @@ bool make_map(CUtensorMap* map, CUtensorMapDataType type, uint32_t size, const v
 }
 
 constexpr uint32_t kMaxPairs = 80;
-constexpr uint32_t kMaxPieces = 160;    // sums of pieces that scratch has room for
+constexpr uint32_t kMaxPieces = 96;     // sums of pieces that scratch has room for
 constexpr uint32_t kMinPieceSteps = 4;  // stages of a piece at the least
 constexpr uint32_t kSumSteps = 12;      // what a piece's sums cost, in stages: 128 KB out of every SM and in again
 
 }  // namespace
 
+// Scratch: the pieces' sums, then the planes of dy, room for up to 8192 rows but at most 64 MB, or for 64 rows if that
+// is more; longer inputs go through in parts.
+static constexpr uint64_t kSumBytes = static_cast<uint64_t>(kMaxPieces) * kWgTile * kWgTile * sizeof(float);
+static uint64_t plane_bytes(uint64_t out_cols) {
+  const uint64_t row = (out_cols + 7) / 8 * 8 * sizeof(__nv_bfloat16) * kPieces<float>;
+  return max(64 * row, min(8192 * row, static_cast<uint64_t>(64) << 20));
+}
 uint64_t act_wgrad_scratch_bytes(uint64_t out_cols, uint64_t cols, uint32_t M) {
-  (void)out_cols, (void)cols, (void)M;
-  return static_cast<uint64_t>(kMaxPieces) * kWgTile * kWgTile * sizeof(float);
+  (void)cols, (void)M;
+  return kSumBytes + plane_bytes(out_cols);
 }
 
-int launch_act_wgrad(int dtype, const WgradArgs& a, const ActView& act, const RowShards& shards, unsigned int* status,
-                     const LaunchShape& shape, cudaStream_t stream) {
-  if (!encode_tiled()) return -1;
+// One part: the rows of `shards`, which dy's planes hold from plane_row0 on.  Workers without rows are left alone
+// unless `zeros`.  -1: refused.
+static int launch_part(int pieces_of_dy, WgradArgs a, const ActView& act, const RowShards& shards, const void* planes, uint64_t ld_planes,
+                       uint64_t plane_row0, uint64_t plane_rows, bool zeros, unsigned int* status, const LaunchShape& shape,
+                       cudaStream_t stream) {
   WgradPlan plan;
   for (uint32_t m = 0; m <= a.M; ++m) plan.row0[m] = static_cast<uint32_t>(shards.row0[m]);
+  plan.plane_row0 = static_cast<uint32_t>(plane_row0);
+  plan.plane_rows = static_cast<uint32_t>(plane_rows);
   plan.tiles_n = (a.out_cols + kWgTile - 1) / kWgTile;
   plan.tiles_k = (act.cols + kWgTile - 1) / kWgTile;
+  uint32_t workers = 0;
   for (uint32_t m = 0; m < a.M; ++m) {  // most rows first: the short ones fill up the last round
-    const uint64_t rows = shards.row0[m + 1] - shards.row0[m];
-    uint32_t i = m;
-    for (; i > 0 && shards.row0[plan.order[i - 1] + 1] - shards.row0[plan.order[i - 1]] < rows; --i) plan.order[i] = plan.order[i - 1];
+    const uint32_t rows = plan.row0[m + 1] - plan.row0[m];
+    if (!rows && !zeros) continue;
+    uint32_t i = workers++;
+    for (; i > 0 && plan.row0[plan.order[i - 1] + 1] - plan.row0[plan.order[i - 1]] < rows; --i) plan.order[i] = plan.order[i - 1];
     plan.order[i] = m;
   }
   const uint32_t pairs = min(kMaxPairs, static_cast<uint32_t>(shape.sm_count / 2));
-  const uint32_t tiles = plan.tiles_n * plan.tiles_k * a.M, left = tiles % pairs;
-  const uint32_t steps = static_cast<uint32_t>((shards.row0[plan.order[0] + 1] - shards.row0[plan.order[0]] + kWgRows - 1) / kWgRows);
+  const uint32_t tiles = plan.tiles_n * plan.tiles_k * workers, left = tiles % pairs;
+  const uint32_t steps = (plan.row0[plan.order[0] + 1] - plan.row0[plan.order[0]] + kWgRows - 1) / kWgRows;
   // The cut that ends soonest: rounds of pieces, each with its stages and, when cut, its sums' way through scratch.
   plan.pieces = 1;
   uint64_t least = steps;
@@ -859,41 +716,69 @@ int launch_act_wgrad(int dtype, const WgradArgs& a, const ActView& act, const Ro
   plan.whole = plan.pieces > 1 ? tiles - left : tiles;
   plan.units = plan.whole + plan.pieces * (tiles - plan.whole);
 
-  WgradArgs args = a;
   const uint64_t all = reinterpret_cast<uintptr_t>(a.g) / 4 | a.ld_w | (a.M > 1 ? a.ld_g : 0);
-  args.vector = all % 4 == 0 ? 4 : all % 2 == 0 ? 2 : 1;
-  const bool tma = dtype != kDtypeF32 && a.ld_dy % 8 == 0 && (reinterpret_cast<uintptr_t>(a.dy) & 15u) == 0;
+  a.vector = all % 4 == 0 ? 4 : all % 2 == 0 ? 2 : 1;
   CUtensorMap map_dy = {}, map_codes = {}, map_exps = {};
   bool ok = true;
   if (act.rows) {  // without rows no copy is issued
     const uint32_t padded = (act.cols + kActBlock - 1) / kActBlock * kActBlock;
-    if (tma) ok &= make_map(&map_dy, dtype == kDtypeF16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, a.dy, a.out_cols, act.rows, a.ld_dy, 64, true);
+    ok &= make_map(&map_dy, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, planes, a.out_cols, plane_rows * pieces_of_dy, ld_planes, 64, true);
     ok &= make_map(&map_codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, act.codes, padded, act.rows, act.ld_codes, kWgHalf, false);
     ok &= make_map(&map_exps, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, act.exps, act.ld_exps, act.rows, act.ld_exps, 16, false);
   }
   if (!ok) return -1;
-  const dim3 grid(2 * min(pairs, plan.units));
-  auto go = [&](auto which, auto kernel, uint32_t smem) {
-    (void)which;  // its type makes this body, and its static, one for each kernel
+  auto go = [&](auto which) {
+    constexpr int kP = decltype(which)::value;
     static std::atomic<uint64_t> prepared{0};  // devices on which this kernel has its shared memory
     const uint64_t device = 1ull << (a.device & 63);
     if (!(prepared.load() & device)) {
       cudaFuncAttributes attributes;
-      ok &= cudaFuncGetAttributes(&attributes, kernel) == cudaSuccess && attributes.numRegs == kLaunchRegs;
-      ok &= cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) == cudaSuccess;
+      ok &= cudaFuncGetAttributes(&attributes, act_wgrad_kernel<kP>) == cudaSuccess && attributes.numRegs == kLaunchRegs;
+      ok &= cudaFuncSetAttribute(act_wgrad_kernel<kP>, cudaFuncAttributeMaxDynamicSharedMemorySize, kWgSmem<kP>) == cudaSuccess;
       if (ok) prepared.fetch_or(device);
     }
-    if (ok) launch_lm(kernel, grid, kWgThreads, smem, 1, stream, shape.chained, map_dy, map_codes, map_exps, plan, args, act.cols, status);
+    if (ok)
+      launch_lm(act_wgrad_kernel<kP>, dim3(2 * min(pairs, plan.units)), kWgThreads, kWgSmem<kP>, 1, stream, shape.chained, map_dy,
+                map_codes, map_exps, plan, a, act.cols, status);
   };
-  if (tma && dtype == kDtypeBf16) go(std::integral_constant<int, 0>(), act_wgrad_kernel<__nv_bfloat16, true>, kWgSmem<__nv_bfloat16, true>);
-  else if (tma) go(std::integral_constant<int, 4>(), act_wgrad_kernel<__half, true>, kWgSmem<__half, true>);
-  else if (dtype == kDtypeBf16) go(std::integral_constant<int, 1>(), act_wgrad_kernel<__nv_bfloat16, false>, kWgSmem<__nv_bfloat16, false>);
-  else if (dtype == kDtypeF16) go(std::integral_constant<int, 2>(), act_wgrad_kernel<__half, false>, kWgSmem<__half, false>);
-  else go(std::integral_constant<int, 3>(), act_wgrad_kernel<float, false>, kWgSmem<float, false>);
+  if (pieces_of_dy == 1) go(std::integral_constant<int, 1>());
+  else if (pieces_of_dy == 2) go(std::integral_constant<int, 2>());
+  else go(std::integral_constant<int, 3>());
   if (!ok) return -1;
   if (plan.pieces == 1) return 1;
   launch_lm(piece_sum_kernel, dim3((tiles - plan.whole) * 32), 256, 0, 1, stream, shape.chained, plan, a, act.cols);
   return 2;
+}
+
+int launch_act_wgrad(int dtype, const WgradArgs& a, const ActView& act, const RowShards& shards, unsigned int* status,
+                     const LaunchShape& shape, cudaStream_t stream) {
+  if (!encode_tiled()) return -1;
+  if (!act.rows || (dtype == kDtypeBf16 && rows_aligned(dtype, a.dy, a.ld_dy)))
+    return launch_part(1, a, act, shards, a.dy, a.ld_dy, 0, act.rows, true, status, shape, stream);
+  int launches = 0;
+  bool ok = true;
+  with_dtype_aligned(dtype, rows_aligned(dtype, a.dy, a.ld_dy), [&](auto t, auto aligned) {
+    using T = decltype(t);
+    constexpr int kP = kPieces<T>;
+    const uint32_t ld = (a.out_cols + 7) / 8 * 8;
+    const uint64_t most = min(act.rows, plane_bytes(a.out_cols) / (ld * sizeof(__nv_bfloat16) * kP) / kWgRows * kWgRows);
+    __nv_bfloat16* planes = reinterpret_cast<__nv_bfloat16*>(static_cast<char*>(a.scratch) + kSumBytes);
+    for (uint64_t row0 = 0; row0 < act.rows && ok; row0 += most) {
+      const uint32_t rows = static_cast<uint32_t>(min(most, act.rows - row0));
+      const uint32_t per_row = (ld + 32 * kSplitUnits * kUnit - 1) / (32 * kSplitUnits * kUnit);
+      launch_lm(split_rows_kernel<T, decltype(aligned)::value>, dim3(static_cast<unsigned>((static_cast<uint64_t>(rows) * per_row + kSplitWarps - 1) / kSplitWarps)),
+                32 * kSplitWarps, 0, 1, stream, shape.chained, static_cast<const T*>(a.dy), a.ld_dy, act.rows, row0, rows, a.out_cols,
+                planes, ld, per_row);
+      RowShards part;
+      for (uint32_t m = 0; m <= kMaxWorkers; ++m) part.row0[m] = min(max(shards.row0[m], row0), row0 + rows);
+      WgradArgs b = a;
+      b.accumulate = a.accumulate || row0 > 0;
+      const int n = launch_part(kP, b, act, part, planes, ld, row0, rows, row0 == 0, status, shape, stream);
+      ok = n > 0;
+      launches += 1 + n;
+    }
+  });
+  return ok ? launches : -1;
 }
 
 }  // namespace qasg
