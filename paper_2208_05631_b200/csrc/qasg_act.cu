@@ -38,10 +38,20 @@ act_pack_kernel(const T* __restrict__ x, uint64_t ld_x, ActView act, uint64_t it
   const ActItem a = act_item(item, per_row);
   const T* row = x + a.row * ld_x;
   const uint32_t padded = (act.cols + kActBlock - 1) & ~static_cast<uint32_t>(kActBlock - 1);
-  const Extent tensor = extent_of(x, act.rows, ld_x, act.cols);
+  const Extent<T> tensor = extent_of(x, act.rows, ld_x, act.cols);
   Fetched<T, kAligned> f[kActItemUnits];
+  if (kAligned && a.col + kActItem <= act.cols) {  // a whole item: nothing to check
+    const Unit<T>* from = reinterpret_cast<const Unit<T>*>(row + a.col) + lane;
 #pragma unroll
-  for (int j = 0; j < kActItemUnits; ++j) f[j] = fetch_unit<T, kAligned>(row, a.row, a.col + (j * 32 + lane) * kUnit, act.cols, tensor);
+    for (int j = 0; j < kActItemUnits; ++j) {
+      const Unit<T> u = load_unit(reinterpret_cast<const T*>(from + j * 32));
+#pragma unroll
+      for (int i = 0; i < static_cast<int>(sizeof(u) / 4); ++i) f[j].w[i] = u.w[i];
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < kActItemUnits; ++j) f[j] = fetch_unit<T, kAligned>(row, a.row, a.col + (j * 32 + lane) * kUnit, act.cols, tensor);
+  }
   bool bad = false;
 #pragma unroll
   for (int j = 0; j < kActItemUnits; ++j) {

@@ -88,15 +88,17 @@ __device__ __forceinline__ void shifted_words(const uint32_t (&x)[kWords + 4], u
   for (int i = 0; i < kWords; ++i) out[i] = __funnelshift_r(z[i], z[i + 1], (shift & 2u) * 8);
 }
 
-// The first byte of a tensor and the one after its last: what may be read.  Eight rows from its ends (16 bytes at the
-// least) the aligned words around a row lie in it.
-struct Extent {
-  const char *lo, *hi;
-  uint64_t inner_rows;  // rows 8 to 8 + inner_rows - 1
+// A tensor of rows: what may be read.  Eight rows from its ends (16 bytes at the least) the aligned words around a row
+// lie in it.
+template <typename T> struct Extent {
+  const T* base;
+  uint64_t rows, ld, cols;
+  __device__ __forceinline__ bool inner(uint64_t row) const { return row >= 8 && row + 8 < rows; }
+  __device__ __forceinline__ const char* lo() const { return reinterpret_cast<const char*>(base); }
+  __device__ __forceinline__ const char* hi() const { return reinterpret_cast<const char*>(base + (rows - 1) * ld + cols); }
 };
-template <typename T> __device__ __forceinline__ Extent extent_of(const T* base, uint64_t rows, uint64_t ld, uint64_t cols) {
-  return {reinterpret_cast<const char*>(base), reinterpret_cast<const char*>(base + (rows - 1) * ld + cols),
-          rows > 16 ? rows - 16 : 0};
+template <typename T> __device__ __forceinline__ Extent<T> extent_of(const T* base, uint64_t rows, uint64_t ld, uint64_t cols) {
+  return {base, rows, ld, cols};
 }
 
 // A unit on its way: fetch_unit() asks for the words, finish_unit() waits for them.  kAligned: every row begins on a
@@ -106,7 +108,7 @@ template <typename T, bool kAligned> struct Fetched { uint32_t w[kUnit * sizeof(
 
 template <typename T, bool kAligned>
 __device__ __forceinline__ Fetched<T, kAligned> fetch_unit(const T* row, uint64_t index, uint32_t c, uint32_t n,
-                                                           const Extent& tensor) {
+                                                           const Extent<T>& tensor) {
   constexpr int kVectors = sizeof(Fetched<T, kAligned>) / 16;
   Fetched<T, kAligned> f;
 #pragma unroll
@@ -114,7 +116,7 @@ __device__ __forceinline__ Fetched<T, kAligned> fetch_unit(const T* row, uint64_
   if (c >= n) return f;
   const char* from = reinterpret_cast<const char*>(row + c);
   from -= kAligned ? 0 : reinterpret_cast<uintptr_t>(from) & 15u;
-  if (kAligned ? c + kUnit <= n : index - 8 < tensor.inner_rows) {
+  if (kAligned ? c + kUnit <= n : tensor.inner(index)) {
 #pragma unroll
     for (int k = 0; k < kVectors; ++k) {
       const uint4* q = reinterpret_cast<const uint4*>(from) + k;
@@ -123,15 +125,16 @@ __device__ __forceinline__ Fetched<T, kAligned> fetch_unit(const T* row, uint64_
     }
     return f;
   }
+  const char *lo = tensor.lo(), *hi = tensor.hi();
 #pragma unroll
   for (int k = 0; k < kVectors; ++k, from += 16) {
-    if (from >= tensor.lo && from + 16 <= tensor.hi) {
+    if (from >= lo && from + 16 <= hi) {
       const uint4 v = *reinterpret_cast<const uint4*>(from);
       f.w[4 * k] = v.x, f.w[4 * k + 1] = v.y, f.w[4 * k + 2] = v.z, f.w[4 * k + 3] = v.w;
     } else {  // the tensor's first or last few values
 #pragma unroll
       for (int i = 0; i < 16; i += sizeof(T)) {
-        if (from + i < tensor.lo || from + i >= tensor.hi) continue;
+        if (from + i < lo || from + i >= hi) continue;
         if (sizeof(T) == 4) f.w[4 * k + i / 4] = *reinterpret_cast<const uint32_t*>(from + i);
         else f.w[4 * k + i / 4] |= static_cast<uint32_t>(*reinterpret_cast<const uint16_t*>(from + i)) << (8 * (i & 2));
       }

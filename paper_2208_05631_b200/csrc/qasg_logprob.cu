@@ -459,7 +459,7 @@ token_logprob_grad_kernel(LogprobGradArgs a, uint32_t per_row, unsigned int* __r
   // p (c0s - c1 y) with y = log2 p
   const float c0s = g_lse - g_lp - (a.g_entropy ? g_h * a.entropy[row] : 0.f), c1 = g_h * kLn2;
   const uint32_t c0 = (part * (kGradThreads * kGradUnits) + threadIdx.x) * kUnit;
-  const Extent tensor = extent_of(static_cast<const T*>(a.logits), a.rows, a.ld, vocab);
+  const Extent<T> tensor = extent_of(static_cast<const T*>(a.logits), a.rows, a.ld, vocab);
   Fetched<T, kAligned> f[kGradUnits];
   if (!zero) {
 #pragma unroll

@@ -45,8 +45,8 @@ rmsnorm_pack_kernel(NormArgs a, ActView act, unsigned int* __restrict__ status) 
   const T* x = static_cast<const T*>(a.x) + row * a.ld_x;
   const T* r = a.residual ? static_cast<const T*>(a.residual) + row * a.ld_r : nullptr;
   Fetched<T, kAligned> fx[kUnits], fr[kUnits];
-  const Extent x_tensor = extent_of(static_cast<const T*>(a.x), act.rows, a.ld_x, cols);
-  const Extent r_tensor = extent_of(static_cast<const T*>(a.residual), act.rows, a.ld_r, cols);
+  const Extent<T> x_tensor = extent_of(static_cast<const T*>(a.x), act.rows, a.ld_x, cols);
+  const Extent<T> r_tensor = extent_of(static_cast<const T*>(a.residual), act.rows, a.ld_r, cols);
 #pragma unroll
   for (int j = 0; j < kUnits; ++j) {
     const uint32_t c = (j * threads + t) * kUnit;
@@ -156,8 +156,8 @@ rmsnorm_grad_kernel(const __grid_constant__ NormGradArgs a, const __grid_constan
   for (int j = 0; j < kUnits; ++j)
 #pragma unroll
     for (int k = 0; k < kUnit; ++k) dw[j][k] = 0.f;
-  const Extent dy_tensor = extent_of(static_cast<const T*>(a.dy), act.rows, a.ld_dy, cols);
-  const Extent dres_tensor = extent_of(static_cast<const T*>(a.dres), act.rows, a.ld_dres, cols);
+  const Extent<T> dy_tensor = extent_of(static_cast<const T*>(a.dy), act.rows, a.ld_dy, cols);
+  const Extent<T> dres_tensor = extent_of(static_cast<const T*>(a.dres), act.rows, a.ld_dres, cols);
   auto dy_row = [&](uint64_t row) { return static_cast<const T*>(a.dy) + row * a.ld_dy; };
   auto dres_row = [&](uint64_t row) { return static_cast<const T*>(a.dres) + row * a.ld_dres; };
   auto fetch = [&](uint64_t row, GradRow<T, kAligned, kUnits>& g) {

@@ -319,7 +319,7 @@ split_rows_kernel(const T* dy, uint64_t ld, uint64_t all_rows, uint64_t row0, ui
   if (row >= rows) return;
   const uint32_t c0 = (static_cast<uint32_t>(item - row * per_row) * 32 * kSplitUnits + (threadIdx.x & 31)) * kUnit;
   const T* from = dy + (row0 + row) * ld;
-  const Extent tensor = extent_of(dy, all_rows, ld, n);
+  const Extent<T> tensor = extent_of(dy, all_rows, ld, n);
   Fetched<T, kAligned> f[kSplitUnits];
 #pragma unroll
   for (int j = 0; j < kSplitUnits; ++j) f[j] = fetch_unit<T, kAligned>(from, row0 + row, c0 + j * 32 * kUnit, n, tensor);
