@@ -404,8 +404,11 @@ qasg_status qasg_act_unpack(qasg_ctx* ctx, const qasg_act* act, qasg_dtype dtype
  *   g          device, fp32; ld_w >= cols, ld_g >= (out_cols-1)*ld_w + cols: row m of a gradient array
  *              [M][ld_g] at the layer's place in it.
  *   accumulate 0: overwrite; else add to what g holds.
- *   scratch    device, 16-byte aligned, qasg_act_wgrad_scratch_bytes(out_cols, cols, M) bytes, which does
- *              not depend on the rows; contents undefined afterwards. */
+ *   scratch    device, 16-byte aligned, qasg_act_wgrad_scratch_bytes(out_cols, cols, M) bytes (at most 88 MiB
+ *              up to 170,000 columns), which does not depend on the rows; contents undefined afterwards.
+ * bf16 rows of dy on 16-byte boundaries are read as they are; any other dy is first rewritten to bf16 planes
+ * in scratch, one (bf16), two (fp16) or three (fp32) of them that add up to its values.  A device-side wait of
+ * this call that runs out is reported as QASG_ERR_TIMEOUT, its gradients are then incomplete. */
 uint64_t qasg_act_wgrad_scratch_bytes(uint64_t out_cols, uint64_t cols, uint32_t M);
 qasg_status qasg_act_wgrad(qasg_ctx* ctx, qasg_dtype dtype, const void* dy, uint64_t ld_dy, uint64_t out_cols,
                            const qasg_act* act, const float* weight, uint32_t M, const uint64_t* shard_row0,

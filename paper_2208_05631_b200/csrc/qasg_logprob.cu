@@ -127,20 +127,23 @@ struct RowShared {
   uint32_t maxima[2][kGroups];  // in value_order
   RowSums warp_sums[32];
   RowSums sums;
-  unsigned int count, unit_count, lost, kept;
+  unsigned int count, lost, kept;
   unsigned long long bound;
 };
 
 // A value that at least k of the groups' maxima reach, within 2^-7 of the largest such: their upper 16 bits are
-// searched bit by bit.  Every warp finds it for itself.
+// searched between the smallest and the largest (seven or eight steps for a row of logits).  Every warp finds it for
+// itself.
 __device__ __forceinline__ float kth_largest(const uint32_t* maxima, uint32_t k) {
-  const uint32_t v0 = maxima[threadIdx.x & 31], v1 = maxima[(threadIdx.x & 31) + 32];
-  uint32_t t = 0;
-#pragma unroll
-  for (uint32_t bit = 1u << 31; bit >= 1u << 16; bit >>= 1) {
-    const uint32_t next = t | bit;
-    if (__popc(__ballot_sync(0xffffffffu, v0 >= next)) + __popc(__ballot_sync(0xffffffffu, v1 >= next)) >= k) t = next;
+  const uint32_t v0 = maxima[threadIdx.x & 31] >> 16, v1 = maxima[(threadIdx.x & 31) + 32] >> 16;
+  uint32_t lo = __reduce_min_sync(0xffffffffu, min(v0, v1)), hi = __reduce_max_sync(0xffffffffu, max(v0, v1));
+  while (lo < hi) {
+    const uint32_t mid = (lo + hi + 1) >> 1;
+    const bool enough = __popc(__ballot_sync(0xffffffffu, v0 >= mid)) + __popc(__ballot_sync(0xffffffffu, v1 >= mid)) >= k;
+    lo = enough ? mid : lo;
+    hi = enough ? hi : mid - 1;
   }
+  const uint32_t t = lo << 16;
   if (t < 0x00800000u) return -INFINITY;
   return t > 0xff800000u ? INFINITY : key_value(static_cast<unsigned long long>(t) << 32);
 }
@@ -176,8 +179,7 @@ __device__ __forceinline__ void cut_list(RowShared& sh, uint32_t k) {
 // Puts the candidates among a thread's units (pending: a bit for each element still to be looked at) on the list;
 // returns the bits of those that found no room.
 template <typename T, int kThreads>
-__device__ __forceinline__ uint32_t push_pending(RowShared& sh, const T* x, uint32_t pending, int64_t c0) {
-  const unsigned long long limit = sh.bound;
+__device__ __forceinline__ uint32_t push_pending(RowShared& sh, const T* x, uint32_t pending, int64_t c0, unsigned long long limit) {
   uint32_t left = 0;
   while (pending) {
     const int b = __ffs(pending) - 1;
@@ -196,7 +198,7 @@ __device__ __forceinline__ uint32_t push_pending(RowShared& sh, const T* x, uint
 template <typename T, int kThreads>
 __device__ __noinline__ void push_round(RowShared& sh, const T* x, uint32_t k, uint32_t pending, int64_t c0) {
   do {
-    pending = push_pending<T, kThreads>(sh, x, pending, c0);
+    pending = push_pending<T, kThreads>(sh, x, pending, c0, sh.bound);
     cut_list<kThreads>(sh, k);
   } while (__syncthreads_or(pending != 0));
 }
@@ -230,7 +232,7 @@ token_logprob_kernel(LogprobArgs a, uint32_t cluster, unsigned int* __restrict__
       return;
     }
   }
-  if (kTop && tid == 0) sh.count = 0, sh.unit_count = 0, sh.lost = 0, sh.bound = 0;
+  if (kTop && tid == 0) sh.count = 0, sh.lost = 0;
   // units on 16-byte boundaries: unit u holds columns 8u - off .. 8u - off + 7
   const uint32_t off = static_cast<uint32_t>((reinterpret_cast<uintptr_t>(x) & 15u) / sizeof(T));
   const uint32_t units = (vocab + off + kUnit - 1) / kUnit, per_part = (units + cluster - 1) / cluster;
@@ -246,6 +248,9 @@ token_logprob_kernel(LogprobArgs a, uint32_t cluster, unsigned int* __restrict__
   uint32_t floor2 = pair_word(T(), -300.f);  // bf16: what is far below m, -inf among it, is raised to about m - 300
   float bound = -INFINITY;
   uint32_t meet = u0, meetings = 0;  // the first unit of the next round after which the bound is taken
+  constexpr uint32_t kWarpList = kListSize / (kThreads / 32);
+  uint32_t* units_of_warp = sh.units + (tid >> 5) * kWarpList;
+  uint32_t noted = 0;
   // Rounds of units: the next one's loads are under way while one is worked on.
   const uint32_t whole = min(u1, (vocab + off) / kUnit);  // units before this one end inside the row; unit 0 may begin before it
   auto is_inside = [&](uint32_t u) { return u > 0 && u + kThreads * kUnits <= whole; };
@@ -291,13 +296,14 @@ token_logprob_kernel(LogprobArgs a, uint32_t cluster, unsigned int* __restrict__
         ++meetings;
         meet = u0 + max(4u * (u - u0), 2u * kThreads * kUnits);
       }
-      if (!(m < bound)) {
+      if (__any_sync(0xffffffffu, !(m < bound))) {
 #pragma unroll
-        for (int j = 0; j < kUnits; ++j)
-          if (!(top[j] < bound)) {
-            const uint32_t w = u + j * kThreads + tid, at = atomicAdd(&sh.unit_count, 1u);
-            if (at < kListSize) sh.units[at] = w;
-          }
+        for (int j = 0; j < kUnits; ++j) {
+          const uint32_t who = __ballot_sync(0xffffffffu, !(top[j] < bound));
+          const uint32_t at = noted + __popc(who & ((1u << (tid & 31)) - 1u));
+          if ((who >> (tid & 31) & 1u) && at < kWarpList) units_of_warp[at] = u + j * kThreads + tid;
+          noted += __popc(who);
+        }
       }
     }
     if (!huge) {
@@ -348,26 +354,28 @@ token_logprob_kernel(LogprobArgs a, uint32_t cluster, unsigned int* __restrict__
     r.s *= c;
   }
   if (kTop) {
-    if (tid == 0) sh.bound = static_cast<unsigned long long>(value_order(bound)) << 32;
-    __syncthreads();
-    bool again = sh.unit_count > kListSize;
-    if (!again) {
-      for (uint32_t i = tid; i < sh.unit_count; i += kThreads) {
-        const uint32_t w = sh.units[i];
+    // every warp looks at the units that it noted
+    const unsigned long long limit = static_cast<unsigned long long>(value_order(bound)) << 32;
+    if (noted > kWarpList) {
+      sh.lost = 1u;
+    } else {
+      __syncwarp();
+      for (uint32_t i = tid & 31; i < noted; i += 32) {
+        const uint32_t w = units_of_warp[i];
         const int64_t c0 = static_cast<int64_t>(w) * kUnit - off;
         float v[kUnit];
         unit_floats(load_ragged_unit<T>(x, c0, vocab), v);
         uint32_t bits = 0;
 #pragma unroll
         for (int k = 0; k < kUnit; ++k) bits |= v[k] < bound || w >= u1 || c0 + k < 0 || c0 + k >= vocab ? 0u : 1u << k;
-        if (push_pending<T, kThreads>(sh, x, bits, c0)) sh.lost = 1u;
+        if (push_pending<T, kThreads>(sh, x, bits, c0, limit)) sh.lost = 1u;
       }
-      __syncthreads();
-      again = sh.lost;
     }
+    __syncthreads();
+    const bool again = sh.lost;
     if (again) {  // too many: once more from the start, cutting the list back to its k best at every round
       __syncthreads();
-      if (tid == 0) sh.count = 0;
+      if (tid == 0) sh.count = 0, sh.bound = limit;
       __syncthreads();
       for (uint32_t u = u0; u < u1; u += kThreads * kUnits) {
         const int64_t c0 = static_cast<int64_t>(u + tid) * kUnit - off;
