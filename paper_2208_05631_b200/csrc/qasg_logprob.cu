@@ -20,6 +20,7 @@ constexpr float kTiny = -160.f;  // 2^kTiny is 0 in fp32: stands for every small
 template <typename T> constexpr int kRoundUnits = sizeof(T) == 4 ? 2 : 4;  // units a thread loads per round: 64 bytes
 constexpr int kListSize = 1024;  // units and elements a CTA has room to note
 constexpr int kMaxCluster = 8;
+constexpr int kManyRows = 128, kFewRows = 512;  // threads of a CTA
 constexpr int kGroups = 64;      // of threads; more than kMaxTop, so that few elements reach the k-th largest maximum
 
 // 2^y within 2 units in the last place; below 2^-126 it is 0.
@@ -204,7 +205,7 @@ __device__ __noinline__ void push_round(RowShared& sh, const T* x, uint32_t k, u
 }
 
 template <typename T, int kThreads, bool kTop>
-__global__ void __launch_bounds__(kThreads, 768 / kThreads)
+__global__ void __launch_bounds__(kThreads, kThreads == kManyRows ? 7 : 1)
 token_logprob_kernel(LogprobArgs a, uint32_t cluster, unsigned int* __restrict__ status) {
   constexpr int kUnits = kRoundUnits<T>;
   __shared__ RowShared sh;
@@ -499,10 +500,9 @@ token_logprob_grad_kernel(LogprobGradArgs a, uint32_t per_row, unsigned int* __r
 }
 
 // ------------------------------------------------------------------ launchers
-constexpr int kManyRows = 128, kFewRows = 512;  // threads of a CTA
 int launch_token_logprob(int dtype, const LogprobArgs& a, unsigned int* status, const LaunchShape& shape,
                          cudaStream_t stream) {
-  // With at least a row for every SM a row is one CTA's, small ones, of which six stand on an SM: their meetings
+  // With at least a row for every SM a row is one CTA's, small ones, of which seven stand on an SM: their meetings
   // cost least.  Fewer rows are split over clusters of large CTAs as long as a CTA keeps a round of loads.
   const bool many = a.rows >= static_cast<uint64_t>(shape.sm_count) || a.vocab <= kManyRows * 32;
   uint32_t cluster = 1;
