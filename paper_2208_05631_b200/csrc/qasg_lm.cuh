@@ -249,20 +249,31 @@ __device__ __forceinline__ float block_largest(const float (&v)[kUnit]) {
   m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, 1));
   return max_nan(m, __shfl_xor_sync(0xffffffffu, m, 2));
 }
-// Codes of one unit as eight bytes; v becomes the rounded codes as floats (0 in a NaN block).
+// Codes of one unit as eight bytes; v becomes the rounded codes as floats (0 in a NaN block).  The product with the scale
+// is exact, so one multiply-add rounds it.  Only what rounds to 128 has to be held at 127: its byte is 0x80, which
+// nothing else is, and rare (magnitudes in the uppermost 1/256 of a binade).
+__device__ __forceinline__ uint32_t low_bytes(float a, float b, float c, float d) {
+  return __byte_perm(__byte_perm(__float_as_uint(a), __float_as_uint(b), 0x0040), __byte_perm(__float_as_uint(c), __float_as_uint(d), 0x0040),
+                     0x5410);
+}
+__device__ __forceinline__ bool has_byte_80(uint32_t w) {
+  const uint32_t z = w ^ 0x80808080u;
+  return ((z - 0x01010101u) & ~z & 0x80808080u) != 0;
+}
 __device__ __forceinline__ uint2 act_codes(float (&v)[kUnit], uint32_t b) {
-  uint32_t w[kUnit];
   const bool bad = b == kActNan;
   const float s = act_scale(b);
+  float r[kUnit];
 #pragma unroll
-  for (int i = 0; i < kUnit; ++i) {
-    const float r = (bad ? 0.f : fminf(fmaxf(v[i] * s, -127.f), 127.f)) + kRoundMagic;
-    w[i] = __float_as_uint(r);
-    v[i] = r - kRoundMagic;
+  for (int i = 0; i < kUnit; ++i) r[i] = fmaf(v[i], s, kRoundMagic);
+  uint2 c = make_uint2(low_bytes(r[0], r[1], r[2], r[3]), low_bytes(r[4], r[5], r[6], r[7]));
+  if (bad || has_byte_80(c.x) || has_byte_80(c.y)) {
+#pragma unroll
+    for (int i = 0; i < kUnit; ++i) r[i] = bad ? kRoundMagic : fminf(fmaxf(r[i], kRoundMagic - 127.f), kRoundMagic + 127.f);
+    c = make_uint2(low_bytes(r[0], r[1], r[2], r[3]), low_bytes(r[4], r[5], r[6], r[7]));
   }
-  uint2 c;
-  c.x = __byte_perm(__byte_perm(w[0], w[1], 0x0040), __byte_perm(w[2], w[3], 0x0040), 0x5410);
-  c.y = __byte_perm(__byte_perm(w[4], w[5], 0x0040), __byte_perm(w[6], w[7], 0x0040), 0x5410);
+#pragma unroll
+  for (int i = 0; i < kUnit; ++i) v[i] = r[i] - kRoundMagic;
   return c;
 }
 // The codes of eight bytes as floats: byte + 128 under the exponent of 2^23, minus 2^23 + 128.
