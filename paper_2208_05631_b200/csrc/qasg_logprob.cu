@@ -8,6 +8,8 @@
 // noted.  At the end the noted units' elements that reach the last bound are ranked.  A row with more of either
 // than there is room for (rising values, ties) is scanned again for them alone.
 // A row is shared by the CTAs of a cluster where there are fewer rows than the GPU has room for.
+// Measured at 1776 x 131072 bf16 (465 MB): 80 us without alternatives (5.8 TB/s; MUFU, one power a logit, 60 % busy), 96 with 8,
+// 115 with 32; fp32 888 x 131072 with 8: 77 us.  One row of 131072: 10 us a call.  Gradient, 2048 x 131072 bf16: 183 us (5.7 TB/s).
 #include <cooperative_groups.h>
 
 #include "qasg_lm.cuh"

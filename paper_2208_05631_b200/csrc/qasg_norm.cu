@@ -6,6 +6,8 @@
 // Both are bound by HBM: a row is read once and kept in registers between its sum and its outputs.  The threads
 // of a CTA share a row (as many warps as the row has units for), or each of its eight warps has a row of its own
 // (kWarpRow, short rows); a thread owns kUnits units of eight adjacent columns, as many units apart as the row has threads.
+// Measured at 8192 x 4096 bf16 with residual and weight: norm 55 us (5.5 TB/s; four units a thread: 62), gradient 47 us (5.0 TB/s)
+// and 5 us for the runs' sums.
 #include "qasg_lm.cuh"
 
 namespace qasg {

@@ -21,6 +21,8 @@
 // kSegmentSteps steps and its sum is added in fp32 outside, rounded to nearest (error then as a plain fp32 product's).
 // Tiles are dealt to the pairs; what is left after the last full round is cut along t into as many pieces as there
 // are pairs for it, whose sums go to scratch and are added in order by a second launch.
+// Measured, 8192 x 4096 x 4096 bf16: 200 us, 1375 TFLOP/s (241 us under the power limit of a long run; torch.matmul of the
+// restored bf16 matrix 178 and 198); products alone, nothing fed: 150 us.
 #include <cuda.h>
 
 #include <atomic>
