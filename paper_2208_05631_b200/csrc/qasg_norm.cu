@@ -111,11 +111,14 @@ rmsnorm_pack_kernel(NormArgs a, ActView act, unsigned int* __restrict__ status) 
 
 // ------------------------------------------------------------------ gradient
 // A CTA takes a run of rows of one worker and keeps their part of the weight gradient in registers; the runs'
-// parts are then added in order by a second launch, so the result does not depend on timing.
+// parts are then added in order by a second launch, so the result does not depend on timing.  Where no worker has more
+// than kDirectRows rows each is one run, and that run's part is the worker's gradient: one launch (a row takes about
+// 2 us, a launch and its part of the call 3).
 struct NormRuns {
   RowShards shards;
   uint32_t run0[kMaxWorkers + 1];  // first run of each worker
   uint32_t rows_per_run;
+  bool direct;  // one run a worker, empty ones included
 };
 
 // What a thread holds of the next row while it works on one.  With more than one unit a thread there is no room for
@@ -231,7 +234,8 @@ rmsnorm_grad_kernel(const __grid_constant__ NormGradArgs a, const __grid_constan
     }
   }
   if (!a.gw) return;
-  float* part = a.partials + static_cast<uint64_t>(blockIdx.x) * ((cols + 7u) & ~7u);
+  float* part = runs.direct ? a.gw + m * a.ld_g : a.partials + static_cast<uint64_t>(blockIdx.x) * ((cols + 7u) & ~7u);
+  const bool add = runs.direct && a.accumulate;
   if (kWarpRow) {
 #pragma unroll
     for (int j = 0; j < kUnits; ++j)
@@ -242,13 +246,20 @@ rmsnorm_grad_kernel(const __grid_constant__ NormGradArgs a, const __grid_constan
       float s = 0.f;
 #pragma unroll
       for (int i = 0; i < kRows; ++i) s += sm_dw[i][c];
-      part[c] = s;
+      part[c] = add ? part[c] + s : s;
     }
   } else {
 #pragma unroll
     for (int j = 0; j < kUnits; ++j) {
       const uint32_t c = (j * threads + t) * kUnit;
-      if (c < cols) store_unit(part + c, pack_unit<float>(dw[j]));  // rows of partials are whole units
+      if (c >= cols) continue;
+      if (!runs.direct) {
+        store_unit(part + c, pack_unit<float>(dw[j]));  // rows of partials are whole units
+      } else {
+#pragma unroll
+        for (int k = 0; k < kUnit; ++k)
+          if (c + k < cols) part[c + k] = add ? part[c + k] + dw[j][k] : dw[j][k];
+      }
     }
   }
 }
@@ -300,7 +311,7 @@ int launch_rmsnorm_pack(int dtype, const NormArgs& a, const ActView& act, unsign
 }
 
 // The gradient keeps a column's sum and weight beside two rows: one unit a thread, four for the widest rows.
-constexpr uint32_t kGradWide = 1024 * kUnit;
+constexpr uint32_t kGradWide = 1024 * kUnit, kDirectRows = 2;
 // Runs of rows: about one for each CTA that 148 SMs hold at 64 registers, plus what the workers' ends add.
 static uint32_t norm_runs(uint32_t cols) {
   const unsigned threads = cols <= 32 * kUnit ? 32 * kWarpRows : row_threads(cols, cols > kGradWide ? 4 : 1);
@@ -319,10 +330,14 @@ int launch_rmsnorm_grad(int dtype, const NormGradArgs& a, const ActView& act, co
   if (act.cols <= 256) runs.rows_per_run = (runs.rows_per_run + 7) / 8 * 8;  // eight rows at a time
   if (!runs.rows_per_run) runs.rows_per_run = 1;
   runs.run0[0] = 0;
+  uint64_t largest = 0;
+  for (uint32_t m = 0; m < a.M; ++m) largest = max(largest, shards.row0[m + 1] - shards.row0[m]);
+  runs.direct = largest <= kDirectRows;
   for (;;) {  // the workers' last runs are short: not one run more than there is room for
+    if (runs.direct) runs.rows_per_run = kDirectRows;
     for (uint32_t m = 0; m < a.M; ++m)
-      runs.run0[m + 1] = runs.run0[m] + static_cast<uint32_t>((shards.row0[m + 1] - shards.row0[m] + runs.rows_per_run - 1) / runs.rows_per_run);
-    if (runs.run0[a.M] <= most || runs.rows_per_run >= rows) break;
+      runs.run0[m + 1] = runs.direct ? m + 1 : runs.run0[m] + static_cast<uint32_t>((shards.row0[m + 1] - shards.row0[m] + runs.rows_per_run - 1) / runs.rows_per_run);
+    if (runs.direct || runs.run0[a.M] <= most || runs.rows_per_run >= rows) break;
     runs.rows_per_run += act.cols <= 256 ? 8 : 1 + runs.rows_per_run / 64;
   }
   int launches = 0;
@@ -339,7 +354,7 @@ int launch_rmsnorm_grad(int dtype, const NormGradArgs& a, const ActView& act, co
     });
     ++launches;
   }
-  if (a.gw) {
+  if (a.gw && !runs.direct) {
     launch_lm(run_sum_kernel, dim3((act.cols + 31) / 32, a.M), 32 * kSumLanes, 0, 1, stream, shape.chained, a.partials, runs,
               act.cols, a.gw, a.ld_g, a.accumulate);
     ++launches;

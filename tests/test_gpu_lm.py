@@ -269,7 +269,8 @@ def test_rmsnorm_gradient_against_differences(ctx):
 WGRAD_SHAPES = [(1, 1, 1, 1, 0, 0), (0, 5, 40, 2, 0, 0), (1, 130, 257, 1, 0, 0), (5, 64, 64, 3, 8, 0), (63, 128, 256, 1, 0, 0),
                 (64, 256, 512, 1, 0, 8), (65, 300, 33, 4, 1, 3), (200, 72, 1000, 7, 0, 0), (513, 512, 256, 2, 0, 0),
                 (1000, 257, 514, 5, 7, 1), (2100, 128, 96, 1, 0, 0), (3000, 40, 2050, 16, 0, 0), (300, 1160, 700, 3, 0, 0),
-                (25000, 20, 33, 4, 1, 0)]   # longer than the scratch holds of dy in another form: in parts
+                (25000, 20, 33, 4, 1, 0),   # longer than the scratch holds of dy in another form: in parts
+                (200, 1500, 3000, 3, 0, 0), (1100, 1500, 3400, 1, 4, 0)]   # several rounds of tiles; the last ones cut in pieces
 
 
 @pytest.mark.parametrize("kind", list(TYPES))
