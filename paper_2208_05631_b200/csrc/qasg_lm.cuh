@@ -111,10 +111,13 @@ __device__ __forceinline__ Fetched<T, kAligned> fetch_unit(const T* row, uint64_
                                                            const Extent<T>& tensor) {
   constexpr int kVectors = sizeof(Fetched<T, kAligned>) / 16;
   Fetched<T, kAligned> f;
+  if (kAligned) {  // (written before the load, the zeros let it be a predicated one)
 #pragma unroll
-  for (int i = 0; i < 4 * kVectors; ++i) f.w[i] = 0u;
-  if (c >= n) return f;
-  const char* from = reinterpret_cast<const char*>(row + c);
+    for (int i = 0; i < 4 * kVectors; ++i) f.w[i] = 0u;
+    if (c >= n) return f;
+  }
+  // off boundaries a lane past the end of the row takes the row's first words: finish_unit() clears them
+  const char* from = reinterpret_cast<const char*>(row + (kAligned || c < n ? c : 0u));
   from -= kAligned ? 0 : reinterpret_cast<uintptr_t>(from) & 15u;
   if (kAligned ? c + kUnit <= n : tensor.inner(index)) {
 #pragma unroll
@@ -124,6 +127,11 @@ __device__ __forceinline__ Fetched<T, kAligned> fetch_unit(const T* row, uint64_
       f.w[4 * k] = v.x, f.w[4 * k + 1] = v.y, f.w[4 * k + 2] = v.z, f.w[4 * k + 3] = v.w;
     }
     return f;
+  }
+  if (!kAligned) {
+#pragma unroll
+    for (int i = 0; i < 4 * kVectors; ++i) f.w[i] = 0u;
+    if (c >= n) return f;
   }
   const char *lo = tensor.lo(), *hi = tensor.hi();
 #pragma unroll
