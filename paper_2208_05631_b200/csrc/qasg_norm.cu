@@ -122,13 +122,18 @@ struct NormRuns {
 };
 
 // What a thread holds of the next row while it works on one.  With more than one unit a thread there is no room for
-// that, and dres and the weights are read where they are used.
+// that: the next row is brought to L2 instead, and dres and the weights are read where they are used.  (4096 rows of bf16
+// with dres: 16384 columns 170 us, 216 with four units a thread and without the L2; 9000 columns, two CTAs an SM, 95 and
+// 210.  Weights in shared memory changed nothing, dres fetched with dy spilled: 183; rows split over clusters: 300 and more,
+// their barrier waits for the stores.)
 template <typename T, bool kAligned, int kUnits> struct GradRow {
   Fetched<T, kAligned> dy[kUnits], dres;
   uint2 codes[kUnits];
   uint32_t exps[kUnits];
   float rstd;
 };
+
+__device__ __forceinline__ void prefetch_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
 
 template <typename T, bool kAligned, bool kWarpRow, int kUnits, int kMaxThreads>
 __global__ void __launch_bounds__(kMaxThreads)
@@ -180,11 +185,24 @@ rmsnorm_grad_kernel(const __grid_constant__ NormGradArgs a, const __grid_constan
       }
     }
   };
+  auto ask_for = [&](uint64_t row) {  // brings a row to L2
+#pragma unroll
+    for (int j = 0; j < kUnits; ++j) {
+      const uint32_t c = (j * threads + t) * kUnit;
+      if (c >= cols) continue;
+      prefetch_l2(dy_row(row) + c);
+      if (a.dres) prefetch_l2(dres_row(row) + c);
+      prefetch_l2(act.codes + row * act.ld_codes + c);
+    }
+  };
   GradRow<T, kAligned, kUnits> g;
   if (kAhead && first + sub < last) fetch(first + sub, g);
   int turn = 0;
   for (uint64_t row = first + sub; row < last; row += kRows, turn ^= 1) {
-    if (!kAhead) fetch(row, g);
+    if (!kAhead) {
+      fetch(row, g);
+      if (row + kRows < last) ask_for(row + kRows);
+    }
     Unit<T> dy[kUnits], dres;
     uint2 codes[kUnits];
     float unit[kUnits];
@@ -310,11 +328,11 @@ int launch_rmsnorm_pack(int dtype, const NormArgs& a, const ActView& act, unsign
   return 1;
 }
 
-// The gradient keeps a column's sum and weight beside two rows: one unit a thread, four for the widest rows.
+// The gradient keeps a column's sum and weight beside two rows: one unit a thread, three for the widest rows.
 constexpr uint32_t kGradWide = 1024 * kUnit, kDirectRows = 2;
 // Runs of rows: about one for each CTA that 148 SMs hold at 64 registers, plus what the workers' ends add.
 static uint32_t norm_runs(uint32_t cols) {
-  const unsigned threads = cols <= 32 * kUnit ? 32 * kWarpRows : row_threads(cols, cols > kGradWide ? 4 : 1);
+  const unsigned threads = cols <= 32 * kUnit ? 32 * kWarpRows : row_threads(cols, cols > kGradWide ? 3 : 1);
   return 148u * (1024u / threads);
 }
 uint64_t rmsnorm_grad_scratch_bytes(uint64_t cols, uint32_t M) {
@@ -352,7 +370,7 @@ int launch_rmsnorm_grad(int dtype, const NormGradArgs& a, const ActView& act, co
       // between 512 and 768 threads an SM holds one CTA at 80 registers as at 64, and 80 spare the spills (1537 x 5003 fp16 38 -> 30 us, 4096 x 5120 fp32 77 -> 54)
       else if (act.cols > 512 * kUnit && act.cols <= 768 * kUnit) go(rmsnorm_grad_kernel<T, kAll, false, 1, 768>, row_threads(act.cols, 1));
       else if (act.cols <= kGradWide) go(rmsnorm_grad_kernel<T, kAll, false, 1, 1024>, row_threads(act.cols, 1));
-      else go(rmsnorm_grad_kernel<T, kAll, false, 4, 512>, row_threads(act.cols, 4));  // up to kNormMaxCols
+      else go(rmsnorm_grad_kernel<T, kAll, false, 3, 704>, row_threads(act.cols, 3));  // up to kNormMaxCols
     });
     ++launches;
   }

@@ -198,7 +198,7 @@ def test_rmsnorm_pack_without_outputs_and_nonfinite(ctx):
 
 
 @pytest.mark.parametrize("kind", list(TYPES))
-@pytest.mark.parametrize("rows,cols,pad,offset", NORM_SHAPES + [(700, 300, 0, 0), (1500, 2048, 0, 0), (160, 5120, 0, 0), (3, 6144, 0, 0), (2, 6145, 0, 0)])
+@pytest.mark.parametrize("rows,cols,pad,offset", NORM_SHAPES + [(700, 300, 0, 0), (1500, 2048, 0, 0), (160, 5120, 0, 0), (3, 6144, 0, 0), (2, 6145, 0, 0), (300, 9000, 0, 0), (150, 16381, 3, 1)])
 def test_rmsnorm_grad(ctx, kind, rows, cols, pad, offset):
     code, dtype = TYPES[kind]
     rng = np.random.default_rng(3 * cols + rows)
