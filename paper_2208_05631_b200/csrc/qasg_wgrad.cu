@@ -53,7 +53,7 @@ constexpr long long kMaxWait = 1ll << 34;                  // bound of every wai
 // dy is read by TMA as one plane of bf16, which takes rows on 16-byte boundaries: its own, if it is bf16 and they are,
 // else planes in scratch that another launch has written, 1 (bf16), 2 (fp16) or 3 (fp32) of them, one below the other.
 // (Shifting and splitting rows inside this kernel, by asynchronous copies and four of the converting warps, took twice
-// as long as both launches: 4031 x 3072 x 2300 fp16 190 us.)
+// as long as both launches: 190 us against 92, 4031 rows and 7.07 M weights, fp16.)
 template <typename T> constexpr int kPieces = 1;
 template <> constexpr int kPieces<__half> = 2;
 template <> constexpr int kPieces<float> = 3;
