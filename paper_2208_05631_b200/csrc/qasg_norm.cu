@@ -25,6 +25,35 @@ __device__ __forceinline__ float row_sum(float v, float* sm) {
   return warp_sum(lane < (blockDim.x >> 5) ? sm[lane] : 0.f);
 }
 
+// The same with the last levels, whose roundings weigh most, in 64 bits.
+template <bool kWarpRow>
+__device__ __forceinline__ double row_sum_wide(float v, float* sm) {
+  const uint32_t lane = threadIdx.x & 31;
+  if (!kWarpRow) {
+    v = warp_sum(v);
+    if (lane == 0) sm[threadIdx.x >> 5] = v;
+    __syncthreads();
+    v = lane < (blockDim.x >> 5) ? sm[lane] : 0.f;
+  }
+  double s = v;
+#pragma unroll
+  for (int i = 16; i; i >>= 1) s += __shfl_xor_sync(~0u, s, i);
+  return s;
+}
+
+// 1 / sqrt(m) as the sum of two floats: a value of n that falls beside the middle of two codes takes the one that its
+// true value takes, where an error of rstd would move a whole row over the middle.  For fp32 rows: two-byte rows come with
+// errors of 2^-9 and 2^-12 of their own, thousands of times as large, and 64-bit steps take them from 55 to 67 us (8192 x 4096 bf16);
+// fp32 rows wait for HBM meanwhile and take as long as without (109 us with the restored values).
+struct Rstd {
+  float hi, lo;
+};
+__device__ __forceinline__ Rstd inverse_root(double m) {
+  const float r = 1.f / sqrtf(static_cast<float>(m));
+  if (!(r > 0.f && r < INFINITY)) return {r, 0.f};
+  return {r, static_cast<float>(0.5 * r * fma(-m, static_cast<double>(r) * r, 1.0))};  // Newton's step
+}
+
 __device__ __forceinline__ void load_weights(const float* __restrict__ weight, uint32_t c, uint32_t cols, float (&w)[kUnit]) {
   if (c + kUnit <= cols && is_aligned16(weight + c)) {
     const float4 a = load_f4(weight + c), b = load_f4(weight + c + 4);
@@ -77,15 +106,17 @@ rmsnorm_pack_kernel(NormArgs a, ActView act, unsigned int* __restrict__ status) 
 #pragma unroll
     for (int j = 0; j < kUnits; ++j) store_row_unit<T, kAligned>(h, (j * threads + t) * kUnit, cols, v[j]);
   }
-  const float rstd = 1.f / sqrtf(row_sum<kWarpRow>(sq, sm) / static_cast<float>(cols) + a.eps);
-  if (t == 0) a.rstd[row] = rstd;
+  Rstd rstd;
+  if constexpr (sizeof(T) == 4) rstd = inverse_root(row_sum_wide<kWarpRow>(sq, sm) / cols + a.eps);
+  else rstd = {1.f / sqrtf(row_sum<kWarpRow>(sq, sm) / static_cast<float>(cols) + a.eps), 0.f};
+  if (t == 0) a.rstd[row] = rstd.hi;
   const uint32_t padded = (cols + kActBlock - 1) & ~static_cast<uint32_t>(kActBlock - 1);
   bool bad = false;
 #pragma unroll
   for (int j = 0; j < kUnits; ++j) {
     const uint32_t c = (j * threads + t) * kUnit;
 #pragma unroll
-    for (int k = 0; k < kUnit; ++k) v[j][k] *= rstd;
+    for (int k = 0; k < kUnit; ++k) v[j][k] = sizeof(T) == 4 ? fmaf(v[j][k], rstd.hi, v[j][k] * rstd.lo) : v[j][k] * rstd.hi;
     const uint32_t b = act_exponent(block_largest(v[j]));
     const uint2 codes = act_codes(v[j], b);
     if (c < padded) {

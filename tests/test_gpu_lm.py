@@ -179,6 +179,20 @@ def test_rmsnorm_pack(ctx, kind, rows, cols, pad, offset):
     assert (np.abs(_f64(y) - want_y) <= (HALF[kind] + EPS) * np.abs(want_y) + TINY[kind]).all()
 
 
+@pytest.mark.parametrize("rows,cols", [(64, 64), (64, 1000), (32, 4096), (8, 9001)])
+def test_rmsnorm_pack_fp32_rounds_like_exact_rows(ctx, rows, cols):
+    # Sums of squares of small whole numbers are exact in fp32, 1 / sqrt is two floats: what is left is one rounding of n.
+    x = torch.from_numpy(np.random.default_rng(cols).integers(-40, 41, (rows, cols)).astype(np.float32)).to(U.dev())
+    rstd = torch.empty(rows, device=U.dev())
+    act = _act(rows, cols)
+    ctx.rmsnorm_pack(TYPES["f32"][0], x, cols, None, 0, None, 0.0, None, 0, None, 0, act, rstd)
+    codes, exps = _act_guards(act)
+    n, _ = O.rmsnorm(_f64(x), 0.0)
+    unit = np.ldexp(1.0, exps.astype(int) - 133).repeat(32, axis=1)[:, :cols]
+    away = np.abs(O.values(codes, exps, cols) - n) - np.where(np.abs(n) > 127 * unit, 1.0, 0.5) * unit
+    assert (away <= 2.0 ** -24 * (1 + 2.0 ** -20) * np.abs(n)).all()
+
+
 def test_rmsnorm_pack_without_outputs_and_nonfinite(ctx):
     rows, cols = 4, 96
     a = np.ones((rows, cols))
